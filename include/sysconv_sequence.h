@@ -1,0 +1,171 @@
+/*
+ * sysconv, sequence operators: causal convolution with carried state, selective state space scan, group norm.
+ * Part of the C ABI of libsysconv.so; conventions, status values and ownership as in sysconv.h.
+ */
+#ifndef SYSCONV_SEQUENCE_H_
+#define SYSCONV_SEQUENCE_H_
+
+#include "sysconv.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ------------------------------------------------------------------------------------------------------------
+ * Sequence operators: what a sequence model puts beside a convolution.  Channels are last and contiguous: a token
+ * is a row of channels.  Token arrays are fp32, bf16 or fp16; every sum, state and statistic is held in fp32 and an
+ * output is rounded to its type once.
+ *
+ * Sequences are DENSE (`sequences` of them, `length` tokens each; token t of sequence r at
+ * ptr + r*batch_stride + t*time_stride) or PACKED (offsets_dev holds sequences+1 ascending numbers, 32 or 64 bits;
+ * token t of sequence r is row offsets[r]+t at ptr + row*time_stride, batch_stride unused; `total` rows in all; `length` is
+ * an upper bound of the longest sequence, total if unknown).  A sequence may be empty.  Offsets outside
+ * [0, total] are clamped, so a wrong one never reads or writes outside the arrays.
+ *
+ * The descriptors below are HOST memory, read before the call returns; every pointer in them is DEVICE memory.
+ * All members are eight bytes wide.  Strides are in elements.  A NULL optional pointer leaves that term out.  Rows
+ * that start 16-byte aligned run faster.  Outputs must not overlap inputs unless stated.  Calls enqueue on `stream`
+ * and do not synchronise; results do not depend on the timing of the device (no floating-point atomics).
+ */
+typedef enum { SYSCONV_T_F32 = 0, SYSCONV_T_BF16 = 1, SYSCONV_T_F16 = 2 } sysconv_type;
+typedef enum { SYSCONV_ACT_NONE = 0, SYSCONV_ACT_SILU = 1 } sysconv_activation;   /* silu(v) = v / (1 + exp(-v)) */
+
+typedef struct {
+    void *ptr;
+    long long batch_stride, time_stride;
+} sysconv_tokens;
+
+typedef struct {
+    long long sequences, length, total;
+    const void *offsets_dev;  /* NULL: dense */
+    long long offsets_64;     /* 1: offsets are 64-bit, 0: 32-bit */
+} sysconv_sequences;
+
+/*
+ * Causal convolution per channel.  With line = state ++ x (the taps-1 inputs before the sequence, then the sequence;
+ * zeros without a state):
+ *   pre[t][c] = bias[c] + sum_{k<taps} weight[c][k] * line[t+k][c],    y = act(pre)
+ * and final_state = the last taps-1 rows of line.  1 <= taps <= 8.
+ * Backward, from y = dL/dy and dfinal = dL/dfinal_state (NULL: zero): dx, dstate, dweight, dbias (each NULL: not wanted).
+ *   weight, bias, dweight, dbias   weight_type: fp32 or the tokens' type; (channels, taps) and (channels), packed
+ *   state, final_state, dfinal, dstate   the tokens' type, (sequences, taps-1, channels), packed
+ *   workspace    of the size sysconv1d_causal_backward_workspace_bytes gives (-1: bad arguments), 16-byte aligned
+ */
+typedef struct {
+    sysconv_sequences seq;
+    long long channels, taps, type, weight_type, activation;
+    sysconv_tokens x, y, dx;
+    const void *weight, *bias, *state;
+    void *final_state;
+    const void *dfinal;
+    void *dstate, *dweight, *dbias;
+    void *workspace;
+    long long workspace_bytes;
+} sysconv_causal_args;
+int sysconv1d_causal(const sysconv_causal_args *args, void *stream);
+long long sysconv1d_causal_backward_workspace_bytes(const sysconv_causal_args *args);
+int sysconv1d_causal_backward(const sysconv_causal_args *args, void *stream);
+
+/*
+ * One token of each of `rows` sequences, whose states are slots of a cache: state is (slots, taps-1, channels), slot s
+ * at state + s*state_stride, and takes the new token in place.  slot_dev (32-bit, may be NULL: row r uses slot r)
+ * names the slot of each row; a row whose slot is outside [0, slots) gives zeros and touches no state.  No two
+ * rows may name the same slot.
+ */
+typedef struct {
+    long long rows, slots, channels, taps, type, weight_type, activation;
+    const void *x;
+    long long x_stride;
+    void *y;
+    long long y_stride;
+    void *state;
+    long long state_stride;
+    const void *weight, *bias, *slot_dev;
+} sysconv_causal_step_args;
+int sysconv1d_causal_step(const sysconv_causal_step_args *args, void *stream);
+
+/*
+ * Selective state space scan.  Per channel c, its group g = c / (channels/groups) and state n:
+ *   d[t]    = delta[t][c] + delta_bias[c], through softplus(v) = log(1 + exp(v)) if `softplus`
+ *   h[t][n] = exp(d[t] A[c][n]) h[t-1][n] + d[t] u[t][c] B[t][g][n]            h[-1] = state (zeros without one)
+ *   y[t][c] = (sum_n C[t][g][n] h[t][n] + D[c] u[t][c]) * silu(z[t][c])
+ * final_state = h after the last token.  1 <= states <= 128; channels a multiple of groups.
+ *   u, delta, z, y (channels per token), B, C (groups*states per token)   tokens of `type`
+ *   A (channels, states), D, delta_bias (channels), state, final_state (sequences, channels, states)   fp32, packed
+ *   saved        NULL, or room for sysscan_saved_blocks() x channels x states fp32: the states at every 16th token,
+ *                which the backward call needs
+ * Backward, from dy = dL/dy and dfinal = dL/dfinal_state: du, ddelta, dz, dB, dC (tokens of `type`), dA, dD, ddelta_bias,
+ * dstate (fp32).  dz needs z; dD, ddelta_bias, dstate may be NULL.
+ *   workspace    of the size sysscan_workspace_bytes / sysscan_backward_workspace_bytes gives (-1: bad arguments),
+ *                16-byte aligned; may be NULL where that is 0
+ */
+typedef struct {
+    sysconv_sequences seq;
+    long long channels, states, groups, type, softplus;
+    sysconv_tokens u, delta, z, B, C, y;
+    const void *A, *D, *delta_bias, *state;
+    void *final_state;
+    void *saved;
+    sysconv_tokens dy, du, ddelta, dz, dB, dC;
+    void *dA, *dD, *ddelta_bias;
+    const void *dfinal;
+    void *dstate;
+    void *workspace;
+    long long workspace_bytes;
+} sysscan_args;
+int sysscan(const sysscan_args *args, void *stream);
+int sysscan_backward(const sysscan_args *args, void *stream);
+long long sysscan_saved_blocks(const sysscan_args *args);
+long long sysscan_workspace_bytes(const sysscan_args *args);
+long long sysscan_backward_workspace_bytes(const sysscan_args *args);
+
+/* One token of each of `rows` sequences; state (slots, channels, states), fp32, slot s at state + s*state_stride, is
+ * updated in place.  Slots as in sysconv1d_causal_step.  Strides: elements between rows. */
+typedef struct {
+    long long rows, slots, channels, states, groups, type, softplus;
+    const void *u;
+    long long u_stride;
+    const void *delta;
+    long long delta_stride;
+    const void *z;
+    long long z_stride;
+    const void *B;
+    long long b_stride;
+    const void *C;
+    long long c_stride;
+    void *y;
+    long long y_stride;
+    const void *A, *D, *delta_bias;
+    void *state;
+    long long state_stride;
+    const void *slot_dev;
+} sysscan_step_args;
+int sysscan_step(const sysscan_step_args *args, void *stream);
+
+/*
+ * Group norm, channels last, with an activation.  x is (batch, space, channels): element (b, s, c) at
+ * x + b*batch_stride + s*space_stride + c (`time_stride` of the token arrays is the space stride).  Over the
+ * space x channels/groups elements of each group of each batch entry:
+ *   y = act((x - mean) * rstd * weight[c] + bias[c]),  rstd = 1 / sqrt(var + eps),  var = mean of (x - mean)^2
+ * weight, bias fp32 or NULL (1 and 0).  mean, rstd: (batch, groups) fp32, written by the forward call (each may be
+ * NULL there), read by the backward call, which gives dx and, where not NULL, dweight and dbias (fp32).
+ *   workspace    as above, of sysgroupnorm_workspace_bytes / sysgroupnorm_backward_workspace_bytes
+ */
+typedef struct {
+    long long batch, space, channels, groups, type, activation;
+    double eps;
+    sysconv_tokens x, y, dy, dx;
+    const void *weight, *bias;
+    void *mean, *rstd, *dweight, *dbias;
+    void *workspace;
+    long long workspace_bytes;
+} sysgroupnorm_args;
+int sysgroupnorm(const sysgroupnorm_args *args, void *stream);
+int sysgroupnorm_backward(const sysgroupnorm_args *args, void *stream);
+long long sysgroupnorm_workspace_bytes(const sysgroupnorm_args *args);
+long long sysgroupnorm_backward_workspace_bytes(const sysgroupnorm_args *args);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* SYSCONV_SEQUENCE_H_ */

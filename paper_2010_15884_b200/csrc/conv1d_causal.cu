@@ -1,0 +1,561 @@
+// Causal convolution per channel with carried state: prompts, backward, single tokens.
+//
+//   pre[t] = bias + sum_{k<K} w[k] line[t+k],  line = state ++ x,  y = act(pre)
+//
+// Bound: memory.  An output costs K multiply-adds and one exp / division pair against 4 bytes (16-bit tokens), so the
+// kernels are built around the traffic: a thread owns V neighbouring channels (16 bytes) and walks along the tokens with
+// the last K-1 inputs in registers, as the output-stationary array does with its forwarded inputs; only a run's first
+// K-1 rows are read twice.  Runs are cut short when there are too few of them to fill the machine.
+#include "seq_common.cuh"
+
+namespace sysconv {
+namespace {
+
+constexpr int kThreads = 128;
+
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&f)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = to_f32(p.v[i]);
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack(const float (&f)[V])
+{
+    Pack<T, V> p;
+#pragma unroll
+    for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(f[i]);
+    return p;
+}
+
+template <typename T>
+__device__ __forceinline__ float load_param(const void *p, long long i, bool f32)
+{
+    return f32 ? static_cast<const float *>(p)[i] : to_f32(static_cast<const T *>(p)[i]);
+}
+
+struct CausalArgs {
+    SeqMap map;
+    Tokens x, y, dx;
+    const void *weight, *bias, *state;
+    void *final_state;
+    const void *dfinal;
+    void *dstate;
+    float *partial;          // backward: [rows][K+1][channels] sums of dweight and dbias
+    int channels, groups;    // groups of V channels
+    int run;                 // tokens per thread
+    long long runs;
+    bool weight_f32, silu;
+};
+
+// Row p of a sequence's line before its first token (p in [-(K-1), 0)), from its state; zeros without one.
+template <typename T, int V, int K>
+__device__ __forceinline__ void load_before(const CausalArgs &a, const void *state, int r, long long p, int c, float (&f)[V])
+{
+    if (state == nullptr) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = 0.0f;
+        return;
+    }
+    const long long row = p < -(K - 1) ? 0 : K - 1 + p;            // a wrong offset cannot lead outside the state
+    unpack(load_pack<T, V>(static_cast<const T *>(state) + (static_cast<long long>(r) * (K - 1) + row) * a.channels + c), f);
+}
+
+// The K-1 inputs before flat token t of sequence r (first token `first`), oldest first.
+template <typename T, int V, int K>
+__device__ __forceinline__ void load_window(const CausalArgs &a, int r, long long first, long long t, int c, float (&win)[K][V])
+{
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+        const long long q = t - (K - 1) + j;
+        if (q >= first) unpack(load_pack<T, V>(token_row<T>(a.x, a.map, r, q) + c), win[j]);
+        else load_before<T, V, K>(a, a.state, r, q - first, c, win[j]);
+    }
+}
+
+template <typename T, int V, int K>
+__device__ __forceinline__ void store_state(const CausalArgs &a, int r, int c, const float (&win)[K][V])
+{
+    if (a.final_state == nullptr) return;
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j)
+        store_pack(static_cast<T *>(a.final_state) + (static_cast<long long>(r) * (K - 1) + j) * a.channels + c, pack<T, V>(win[j]));
+}
+
+// The final state of every empty sequence from r on whose place is flat token t; returns the first sequence that is not.
+template <typename T, int V, int K>
+__device__ __forceinline__ int pass_empty(const CausalArgs &a, int r, long long t, int c)
+{
+    while (r < a.map.sequences && a.map.end(r) <= t) {
+        float win[K][V];
+        load_window<T, V, K>(a, r, t, t, c, win);
+        store_state<T, V, K>(a, r, c, win);
+        ++r;
+    }
+    return r;
+}
+
+template <typename T, int V, int K>
+__global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
+{
+    dependent_launch_enter();
+    constexpr int U = 4;                                            // tokens in flight per thread
+    const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    const long long run = id / a.groups;
+    if (run >= a.runs) return;
+    const int c = static_cast<int>(id - run * a.groups) * V;
+    long long t = run * a.run;
+    const long long stop = min(t + a.run, a.map.total);
+
+    float w[K][V], bias[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) w[k][i] = load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32);
+        bias[i] = a.bias ? load_param<T>(a.bias, c + i, a.weight_f32) : 0.0f;
+    }
+    int r = t == 0 ? pass_empty<T, V, K>(a, 0, 0, c) : a.map.find(t);
+    while (t < stop && r < a.map.sequences) {
+        const long long first = a.map.first(r), end = a.map.end(r);
+        const long long last = min(end, stop);
+        float win[K][V];                                            // the K-1 inputs before t; win[K-1]: the input of t
+        load_window<T, V, K>(a, r, first, t, c, win);
+        const T *src = token_row<T>(a.x, a.map, r, t) + c;
+        T *dst = token_row<T>(a.y, a.map, r, t) + c;
+        while (t < last) {
+            const int n = static_cast<int>(min(last - t, static_cast<long long>(U)));
+            Pack<T, V> raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < n) raw[u] = load_pack<T, V>(src + u * a.x.tstride);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u < n) {
+                    unpack(raw[u], win[K - 1]);
+                    float out[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float v = bias[i];
+#pragma unroll
+                        for (int k = 0; k < K; ++k) v = fmaf(w[k][i], win[k][i], v);
+                        out[i] = a.silu ? silu(v) : v;
+                    }
+                    store_pack(dst + u * a.y.tstride, pack<T, V>(out));
+#pragma unroll
+                    for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
+                }
+            }
+            t += n;
+            src += n * a.x.tstride;
+            dst += n * a.y.tstride;
+        }
+        if (t >= end) {                                             // (t > end: descending offsets; never loop on them)
+            store_state<T, V, K>(a, r, c, win);
+            r = pass_empty<T, V, K>(a, r + 1, t, c);
+        }
+    }
+}
+
+// Backward.  A run's thread walks its tokens forwards: dpre[t] = dy[t] act'(pre[t]) needs the same window as the forward
+// pass, and the last K of them give dx[t-(K-1)] = sum_k w[k] dpre[t-k], so both windows live in registers and a token's
+// x and dy are read once (the K-1 tokens behind a run a second time).  The sums for dweight and dbias stay in registers
+// over the run, are added over the block's runs in shared memory and leave as one partial row per block row; a second
+// kernel adds the rows in a fixed order.
+constexpr int kBackRows = 4;             // runs per block, 32 threads (groups of V channels) each
+
+template <typename T, int V, int K>
+__global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalArgs a)
+{
+    dependent_launch_enter();
+    const int group = blockIdx.x * 32 + threadIdx.x;
+    const long long run = static_cast<long long>(blockIdx.y) * kBackRows + threadIdx.y;
+    const bool live = group < a.groups && run < a.runs;
+    const int c = live ? group * V : 0;
+    float w[K][V], bias[V], dw[K][V], db[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            w[k][i] = load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32);
+            dw[k][i] = 0.0f;
+        }
+        bias[i] = a.bias ? load_param<T>(a.bias, c + i, a.weight_f32) : 0.0f;
+        db[i] = 0.0f;
+    }
+    if (live) {
+        const long long start = run * a.run, stop = min(start + a.run, a.map.total);
+        long long t = start;
+        int r = t == 0 ? 0 : a.map.find(t);
+        // dL/dline row s of sequence r (s < 0: state): `sum` and what comes through the final state
+        auto emit = [&](int rr, long long first, long long end, long long s, float (&f)[V]) {
+            if (a.dfinal != nullptr && s >= end - (K - 1)) {
+                float g[V];
+                unpack(load_pack<T, V>(static_cast<const T *>(a.dfinal) +
+                                       (static_cast<long long>(rr) * (K - 1) + (s - end + K - 1)) * a.channels + c), g);
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] += g[i];
+            }
+            if (s >= first) {
+                if (a.dx.ptr != nullptr) store_pack(token_row<T>(a.dx, a.map, rr, s) + c, pack<T, V>(f));
+            } else if (a.dstate != nullptr) {
+                store_pack(static_cast<T *>(a.dstate) + (static_cast<long long>(rr) * (K - 1) + (s - first + K - 1)) * a.channels + c,
+                           pack<T, V>(f));
+            }
+        };
+        auto pass_empty_back = [&](int rr, long long at) {
+            while (rr < a.map.sequences && a.map.end(rr) <= at) {
+                for (int j = 0; j < K - 1; ++j) {
+                    float f[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) f[i] = 0.0f;
+                    emit(rr, at, at, at - (K - 1) + j, f);
+                }
+                ++rr;
+            }
+            return rr;
+        };
+        if (t == 0) r = pass_empty_back(0, 0);
+        while (t < stop && r < a.map.sequences) {
+            const long long first = a.map.first(r), end = a.map.end(r), start_t = t;
+            const long long mine = min(end, stop);                   // tokens whose sums and dx are this run's
+            const long long last = min(end, mine + K - 1);           // tokens whose dpre they need
+            const long long from = t > first ? t : first - (K - 1);  // line rows that are this run's
+            float win[K][V], g[K][V];                                // g[k]: dpre of token t-k
+            load_window<T, V, K>(a, r, first, t, c, win);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[k][i] = 0.0f;
+            const T *src = token_row<T>(a.x, a.map, r, t) + c;
+            const T *dsrc = token_row<T>(a.y, a.map, r, t) + c;
+            constexpr int U = 2;
+            const long long flush = end <= mine + K - 1 ? end + K - 1 : last;   // past the end dpre is zero
+            while (t < flush) {
+                const int n = static_cast<int>(min(flush - t, static_cast<long long>(U)));
+                Pack<T, V> xr[U], yr[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (t + u < last) {
+                        xr[u] = load_pack<T, V>(src + u * a.x.tstride);
+                        yr[u] = load_pack<T, V>(dsrc + u * a.y.tstride);
+                    }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (u < n) {
+                        if (t + u < last) {
+                            float dy[V];
+                            unpack(xr[u], win[K - 1]);
+                            unpack(yr[u], dy);
+#pragma unroll
+                            for (int i = 0; i < V; ++i) {
+                                float v = bias[i];
+#pragma unroll
+                                for (int k = 0; k < K; ++k) v = fmaf(w[k][i], win[k][i], v);
+                                const float d = a.silu ? dy[i] * silu_slope(v, sigmoid(v)) : dy[i];
+                                g[0][i] = d;
+                                if (t + u < mine) {
+                                    db[i] += d;
+#pragma unroll
+                                    for (int k = 0; k < K; ++k) dw[k][i] = fmaf(d, win[k][i], dw[k][i]);
+                                }
+                            }
+#pragma unroll
+                            for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                                for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
+                        }
+                        const long long s = t + u - (K - 1);
+                        if (s >= from && s < mine) {
+                            float f[V];
+#pragma unroll
+                            for (int i = 0; i < V; ++i) {
+                                f[i] = 0.0f;
+#pragma unroll
+                                for (int k = 0; k < K; ++k) f[i] = fmaf(w[k][i], g[k][i], f[i]);
+                            }
+                            emit(r, first, end, s, f);
+                        }
+#pragma unroll
+                        for (int k = K - 1; k > 0; --k)
+#pragma unroll
+                            for (int i = 0; i < V; ++i) g[k][i] = g[k - 1][i];
+                    }
+                }
+                t += n;
+                src += n * a.x.tstride;
+                dsrc += n * a.y.tstride;
+            }
+            t = max(start_t, mine);                                  // (mine < start_t: descending offsets)
+            if (t >= end) r = pass_empty_back(r + 1, t);
+        }
+    }
+    if (a.partial == nullptr) return;
+    __shared__ float sums[kBackRows][(K + 1) * V][33];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) sums[threadIdx.y][k * V + i][threadIdx.x] = dw[k][i];
+        sums[threadIdx.y][K * V + i][threadIdx.x] = db[i];
+    }
+    __syncthreads();
+    for (int e = threadIdx.y * 32 + threadIdx.x; e < (K + 1) * V * 32; e += 32 * kBackRows) {
+        const int k = e / (32 * V), ch = e % (32 * V);              // channel within the block's 32 groups
+        const int gc = blockIdx.x * 32 * V + ch;
+        if (gc < a.channels) {
+            float v = 0.0f;
+#pragma unroll
+            for (int y = 0; y < kBackRows; ++y) v += sums[y][k * V + ch % V][ch / V];
+            a.partial[(static_cast<long long>(blockIdx.y) * (K + 1) + k) * a.channels + gc] = v;
+        }
+    }
+}
+
+// dweight and dbias: column sums of the partial rows.  A block takes 32 columns (of (K+1) x channels) and 32 row slices.
+template <typename W>
+__global__ void __launch_bounds__(1024) causal_reduce_kernel(const float *partial, long long rows, int channels, int taps, W *dweight, W *dbias)
+{
+    dependent_launch_enter();
+    __shared__ float sums[32][33];
+    const long long columns = static_cast<long long>(taps + 1) * channels;
+    const long long col = static_cast<long long>(blockIdx.x) * 32 + threadIdx.x;
+    float v = 0.0f;
+    if (col < columns)
+        for (long long r = threadIdx.y; r < rows; r += 32) v += partial[r * columns + col];
+    sums[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.y != 0 || col >= columns) return;
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += sums[i][threadIdx.x];
+    const int k = static_cast<int>(col / channels), c = static_cast<int>(col % channels);
+    if (k < taps) {
+        if (dweight != nullptr) dweight[static_cast<long long>(c) * taps + k] = from_f32<W>(v);
+    } else if (dbias != nullptr) {
+        dbias[c] = from_f32<W>(v);
+    }
+}
+
+// Single tokens: one thread per row and V channels.
+struct CausalStepArgs {
+    const void *x, *weight, *bias;
+    void *y, *state;
+    const int *slot;
+    long long x_stride, y_stride, state_stride, rows, slots;
+    int channels, groups;
+    bool weight_f32, silu;
+};
+
+template <typename T, int V, int K>
+__global__ void __launch_bounds__(kThreads) causal_step_kernel(CausalStepArgs a)
+{
+    dependent_launch_enter();
+    const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    const long long row = id / a.groups;
+    if (row >= a.rows) return;
+    const int c = static_cast<int>(id - row * a.groups) * V;
+    const long long slot = a.slot ? a.slot[row] : row;
+    T *dst = static_cast<T *>(a.y) + row * a.y_stride + c;
+    float out[V];
+    if (slot < 0 || slot >= a.slots) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = 0.0f;
+        store_pack(dst, pack<T, V>(out));
+        return;
+    }
+    T *st = static_cast<T *>(a.state) + slot * a.state_stride + c;
+    Pack<T, V> line[K];
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) line[k] = load_pack<T, V>(st + static_cast<long long>(k) * a.channels);
+    line[K - 1] = load_pack<T, V>(static_cast<const T *>(a.x) + row * a.x_stride + c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        float v = a.bias ? load_param<T>(a.bias, c + i, a.weight_f32) : 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            v = fmaf(load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32), to_f32(line[k].v[i]), v);
+        out[i] = a.silu ? silu(v) : v;
+    }
+    store_pack(dst, pack<T, V>(out));
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) store_pack(st + static_cast<long long>(k) * a.channels, line[k + 1]);
+}
+
+// ---- dispatch -----------------------------------------------------------------------------------------------------
+
+template <int K> struct Taps { static constexpr int value = K; };
+template <typename F>
+cudaError_t with_taps(long long k, F f)
+{
+    switch (k) {
+        case 1: return f(Taps<1>{});
+        case 2: return f(Taps<2>{});
+        case 3: return f(Taps<3>{});
+        case 4: return f(Taps<4>{});
+        case 5: return f(Taps<5>{});
+        case 6: return f(Taps<6>{});
+        case 7: return f(Taps<7>{});
+        case 8: return f(Taps<8>{});
+        default: return kNoInstantiation;
+    }
+}
+
+// channels per thread of the 128-bit form; fewer for long filters, whose windows would not fit the registers
+template <typename T, int K>
+constexpr int wide_forward() { return sizeof(T) == 2 && K <= 4 ? 8 : 4; }
+
+CausalArgs base_args(const sysconv_causal_args &a)
+{
+    CausalArgs k = {};
+    k.map = make_seq_map(a.seq);
+    k.x = make_tokens(a.x);
+    k.y = make_tokens(a.y);
+    k.dx = make_tokens(a.dx);
+    k.weight = a.weight;
+    k.bias = a.bias;
+    k.state = a.state;
+    k.final_state = a.final_state;
+    k.dfinal = a.dfinal;
+    k.dstate = a.dstate;
+    k.channels = static_cast<int>(a.channels);
+    k.weight_f32 = a.weight_type == SYSCONV_T_F32;
+    k.silu = a.activation == SYSCONV_ACT_SILU;
+    return k;
+}
+
+// Tokens per run: as long as there are `threads` of them at work, at most `most`.
+int run_length(long long total, long long groups, long long threads, int most)
+{
+    const long long n = total * groups / threads;
+    return static_cast<int>(n < 1 ? 1 : (n > most ? most : n));
+}
+
+bool state_aligned(const sysconv_causal_args &a, size_t esz, size_t bytes)
+{
+    return a.channels * esz % bytes == 0 && ptr_aligned(a.state, bytes) && ptr_aligned(a.final_state, bytes) &&
+           ptr_aligned(a.dfinal, bytes) && ptr_aligned(a.dstate, bytes);
+}
+
+long long backward_runs(const sysconv_causal_args &a, int v, int *run)
+{
+    const long long total = a.seq.offsets_dev ? a.seq.total : a.seq.sequences * a.seq.length;
+    const long long groups = (a.channels + v - 1) / v;
+    *run = run_length(total, groups, 148LL * 1024, 128);
+    const long long least = total / (65535LL * kBackRows) + 1;          // the grid's rows are limited
+    if (*run < least) *run = static_cast<int>(least);
+    const long long runs = (total + *run - 1) / *run;
+    return runs < 1 ? 1 : runs;
+}
+
+bool backward_wide(const sysconv_causal_args &a)
+{
+    const size_t esz = a.type == SYSCONV_T_F32 ? 4 : 2;
+    const bool packed = a.seq.offsets_dev != nullptr;
+    return rows_aligned(a.x, packed, esz, 4 * esz) && rows_aligned(a.y, packed, esz, 4 * esz) &&
+           (a.dx.ptr == nullptr || rows_aligned(a.dx, packed, esz, 4 * esz)) && state_aligned(a, esz, 4 * esz);
+}
+
+}  // namespace
+
+cudaError_t launch_causal(const sysconv_causal_args &a, cudaStream_t s, int *launches)
+{
+    return with_type(a.type, [&](auto *tag) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        return with_taps(a.taps, [&](auto taps) {
+            constexpr int K = decltype(taps)::value;
+            constexpr int V = wide_forward<T, K>();
+            const bool packed = a.seq.offsets_dev != nullptr;
+            const size_t bytes = V * sizeof(T);
+            const bool wide = rows_aligned(a.x, packed, sizeof(T), bytes) && rows_aligned(a.y, packed, sizeof(T), bytes) &&
+                              state_aligned(a, sizeof(T), bytes);
+            CausalArgs k = base_args(a);
+            k.groups = wide ? k.channels / V : k.channels;
+            k.run = run_length(k.map.total, k.groups, 148LL * 1024, 16);
+            k.runs = k.map.total > 0 ? (k.map.total + k.run - 1) / k.run : 1;
+            const long long blocks = (k.runs * k.groups + kThreads - 1) / kThreads;
+            if (blocks > 0x7fffffffLL) return kNoInstantiation;
+            *launches += 1;
+            return wide ? launch_kernel(causal_kernel<T, V, K>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), s, k)
+                        : launch_kernel(causal_kernel<T, 1, K>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), s, k);
+        });
+    });
+}
+
+long long causal_backward_workspace(const sysconv_causal_args &a)
+{
+    if (a.dweight == nullptr && a.dbias == nullptr) return 0;
+    int run;
+    const long long runs = backward_runs(a, backward_wide(a) ? 4 : 1, &run);
+    return (runs + kBackRows - 1) / kBackRows * (a.taps + 1) * a.channels * 4;
+}
+
+cudaError_t launch_causal_backward(const sysconv_causal_args &a, cudaStream_t s, int *launches)
+{
+    const bool wide = backward_wide(a);
+    CausalArgs k = base_args(a);
+    k.groups = wide ? k.channels / 4 : k.channels;
+    k.runs = backward_runs(a, wide ? 4 : 1, &k.run);
+    const bool params = a.dweight != nullptr || a.dbias != nullptr;
+    k.partial = params ? static_cast<float *>(a.workspace) : nullptr;
+    const long long rows = (k.runs + kBackRows - 1) / kBackRows;
+    if (rows > 65535) return kNoInstantiation;
+    cudaError_t err = with_type(a.type, [&](auto *tag) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        return with_taps(a.taps, [&](auto taps) {
+            constexpr int K = decltype(taps)::value;
+            const dim3 grid(ceil_div(k.groups, 32), static_cast<unsigned>(rows)), block(32, kBackRows);
+            *launches += 1;
+            return wide ? launch_kernel(causal_backward_kernel<T, 4, K>, grid, block, s, k)
+                        : launch_kernel(causal_backward_kernel<T, 1, K>, grid, block, s, k);
+        });
+    });
+    if (err != cudaSuccess || !params) return err;
+    const dim3 grid(ceil_div((a.taps + 1) * a.channels, 32)), block(32, 32);
+    *launches += 1;
+    const int taps = static_cast<int>(a.taps);
+    return with_type(a.weight_type, [&](auto *tag) {
+        using W = std::remove_pointer_t<decltype(tag)>;
+        return launch_kernel(causal_reduce_kernel<W>, grid, block, s, k.partial, rows, k.channels, taps, static_cast<W *>(a.dweight),
+                             static_cast<W *>(a.dbias));
+    });
+}
+
+cudaError_t launch_causal_step(const sysconv_causal_step_args &a, cudaStream_t s, int *launches)
+{
+    return with_type(a.type, [&](auto *tag) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        return with_taps(a.taps, [&](auto taps) {
+            constexpr int K = decltype(taps)::value;
+            constexpr int V = 8 / sizeof(T);                        // few rows: 8 bytes a thread, twice the threads
+            CausalStepArgs k = {};
+            k.x = a.x;
+            k.y = a.y;
+            k.state = a.state;
+            k.weight = a.weight;
+            k.bias = a.bias;
+            k.slot = static_cast<const int *>(a.slot_dev);
+            k.x_stride = a.x_stride;
+            k.y_stride = a.y_stride;
+            k.state_stride = a.state_stride;
+            k.rows = a.rows;
+            k.slots = a.slots;
+            k.channels = static_cast<int>(a.channels);
+            k.weight_f32 = a.weight_type == SYSCONV_T_F32;
+            k.silu = a.activation == SYSCONV_ACT_SILU;
+            const bool wide = a.channels % V == 0 && a.x_stride % V == 0 && a.y_stride % V == 0 && a.state_stride % V == 0 &&
+                              ptr_aligned(a.x, 8) && ptr_aligned(a.y, 8) && ptr_aligned(a.state, 8);
+            k.groups = wide ? k.channels / V : k.channels;
+            const long long blocks = (k.rows * k.groups + kThreads - 1) / kThreads;
+            if (blocks > 0x7fffffffLL) return kNoInstantiation;
+            *launches += 1;
+            return wide ? launch_kernel(causal_step_kernel<T, V, K>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), s, k)
+                        : launch_kernel(causal_step_kernel<T, 1, K>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), s, k);
+        });
+    });
+}
+
+}  // namespace sysconv

@@ -1,0 +1,222 @@
+// C ABI of the sequence operators: argument checks and dispatch.  See include/sysconv_sequence.h for the contract.
+#include "seq_common.cuh"
+
+namespace {
+
+using namespace sysconv;
+
+bool valid_type(long long t) { return t >= SYSCONV_T_F32 && t <= SYSCONV_T_F16; }
+
+constexpr long long kMaxTokens = 1LL << 40;
+
+int check_sequences(const sysconv_sequences &s)
+{
+    if (s.sequences < 1 || s.length < 0) return SYSCONV_EINVAL;
+    if (s.offsets_dev != nullptr && s.total < 0) return SYSCONV_EINVAL;
+    if (s.sequences > (1LL << 30) || s.length > kMaxTokens || s.total > kMaxTokens || s.length > kMaxTokens / s.sequences * 2)
+        return SYSCONV_EUNSUPPORTED;
+    return SYSCONV_OK;
+}
+
+long long tokens_of(const sysconv_sequences &s) { return s.offsets_dev ? s.total : s.sequences * s.length; }
+
+// Token array with `row` contiguous elements per token.  Inputs may repeat rows (stride 0); outputs may not.
+bool valid_tokens(const sysconv_tokens &t, const sysconv_sequences &s, long long row, bool output)
+{
+    if (tokens_of(s) == 0) return true;                       // nothing is read or written
+    if (t.ptr == nullptr || t.time_stride < 0 || t.batch_stride < 0) return false;
+    if (!output) return true;
+    if (s.offsets_dev != nullptr) return s.total <= 1 || t.time_stride >= row;
+    return (s.length <= 1 || t.time_stride >= row) && (s.sequences <= 1 || t.batch_stride >= row);
+}
+
+int check_causal(const sysconv_causal_args *a, bool backward)
+{
+    if (a == nullptr) return SYSCONV_EINVAL;
+    int st = check_sequences(a->seq);
+    if (st != SYSCONV_OK) return st;
+    if (a->channels < 1 || a->taps < 1 || !valid_type(a->type) || !a->weight) return SYSCONV_EINVAL;
+    if (a->weight_type != SYSCONV_T_F32 && a->weight_type != a->type) return SYSCONV_EINVAL;
+    if (a->activation != SYSCONV_ACT_NONE && a->activation != SYSCONV_ACT_SILU) return SYSCONV_EINVAL;
+    if (a->taps > 8 || a->channels > (1LL << 28)) return SYSCONV_EUNSUPPORTED;
+    if (!valid_tokens(a->x, a->seq, a->channels, false) || !valid_tokens(a->y, a->seq, a->channels, !backward)) return SYSCONV_EINVAL;
+    if (backward && a->dx.ptr != nullptr && !valid_tokens(a->dx, a->seq, a->channels, true)) return SYSCONV_EINVAL;
+    return SYSCONV_OK;
+}
+
+int check_scan(const sysscan_args *a, bool backward)
+{
+    if (a == nullptr) return SYSCONV_EINVAL;
+    int st = check_sequences(a->seq);
+    if (st != SYSCONV_OK) return st;
+    if (a->channels < 1 || a->states < 1 || a->groups < 1 || a->channels % a->groups != 0 || !valid_type(a->type) || !a->A)
+        return SYSCONV_EINVAL;
+    if (a->states > kMaxStates || a->seq.sequences > 65535 || a->channels > (1LL << 30) / a->states) return SYSCONV_EUNSUPPORTED;
+    const long long bc = a->groups * a->states;
+    if (!valid_tokens(a->u, a->seq, a->channels, false) || !valid_tokens(a->delta, a->seq, a->channels, false) ||
+        !valid_tokens(a->B, a->seq, bc, false) || !valid_tokens(a->C, a->seq, bc, false))
+        return SYSCONV_EINVAL;
+    if (a->z.ptr != nullptr && !valid_tokens(a->z, a->seq, a->channels, false)) return SYSCONV_EINVAL;
+    if (!backward) return valid_tokens(a->y, a->seq, a->channels, true) ? SYSCONV_OK : SYSCONV_EINVAL;
+    if (!valid_tokens(a->dy, a->seq, a->channels, false) || !valid_tokens(a->du, a->seq, a->channels, true) ||
+        !valid_tokens(a->ddelta, a->seq, a->channels, true) || !valid_tokens(a->dB, a->seq, bc, true) ||
+        !valid_tokens(a->dC, a->seq, bc, true))
+        return SYSCONV_EINVAL;
+    if (a->z.ptr != nullptr && !valid_tokens(a->dz, a->seq, a->channels, true)) return SYSCONV_EINVAL;
+    if ((a->saved == nullptr && tokens_of(a->seq) > 0) || a->dA == nullptr) return SYSCONV_EINVAL;
+    return SYSCONV_OK;
+}
+
+int check_norm(const sysgroupnorm_args *a, bool backward)
+{
+    if (a == nullptr) return SYSCONV_EINVAL;
+    if (a->batch < 1 || a->space < 1 || a->channels < 1 || a->groups < 1 || a->channels % a->groups != 0 || !valid_type(a->type) ||
+        !(a->eps >= 0.0))
+        return SYSCONV_EINVAL;
+    if (a->activation != SYSCONV_ACT_NONE && a->activation != SYSCONV_ACT_SILU) return SYSCONV_EINVAL;
+    if (a->channels > (1LL << 28) || a->space > kMaxTokens || a->batch > kMaxTokens / a->space) return SYSCONV_EUNSUPPORTED;
+    const sysconv_sequences s = {a->batch, a->space, 0, nullptr, 0};
+    if (!valid_tokens(a->x, s, a->channels, false)) return SYSCONV_EINVAL;
+    if (!backward) return valid_tokens(a->y, s, a->channels, true) ? SYSCONV_OK : SYSCONV_EINVAL;
+    if (!valid_tokens(a->dy, s, a->channels, false) || !valid_tokens(a->dx, s, a->channels, true) || !a->mean || !a->rstd)
+        return SYSCONV_EINVAL;
+    return SYSCONV_OK;
+}
+
+bool valid_workspace(void *p, long long have, long long need)
+{
+    return need == 0 || (need > 0 && p != nullptr && have >= need && ptr_aligned(p, 16));
+}
+
+// launches by reference: the argument `err` is what counts them
+int done(cudaError_t err, const int &launches)
+{
+    if (err == kNoInstantiation) return SYSCONV_EUNSUPPORTED;
+    if (err != cudaSuccess) return SYSCONV_ECUDA;
+    count_launches(launches);
+    return SYSCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sysconv1d_causal(const sysconv_causal_args *a, void *stream)
+{
+    const int st = check_causal(a, false);
+    if (st != SYSCONV_OK) return st;
+    int launches = 0;
+    return done(launch_causal(*a, static_cast<cudaStream_t>(stream), &launches), launches);
+}
+
+long long sysconv1d_causal_backward_workspace_bytes(const sysconv_causal_args *a)
+{
+    return check_causal(a, true) == SYSCONV_OK ? causal_backward_workspace(*a) : -1;
+}
+
+int sysconv1d_causal_backward(const sysconv_causal_args *a, void *stream)
+{
+    const int st = check_causal(a, true);
+    if (st != SYSCONV_OK) return st;
+    if (!valid_workspace(a->workspace, a->workspace_bytes, causal_backward_workspace(*a))) return SYSCONV_EINVAL;
+    int launches = 0;
+    return done(launch_causal_backward(*a, static_cast<cudaStream_t>(stream), &launches), launches);
+}
+
+int sysconv1d_causal_step(const sysconv_causal_step_args *a, void *stream)
+{
+    if (a == nullptr || a->rows < 1 || a->slots < 0 || a->channels < 1 || a->taps < 1 || !valid_type(a->type) || !a->x || !a->y || !a->weight)
+        return SYSCONV_EINVAL;
+    if (a->weight_type != SYSCONV_T_F32 && a->weight_type != a->type) return SYSCONV_EINVAL;
+    if (a->activation != SYSCONV_ACT_NONE && a->activation != SYSCONV_ACT_SILU) return SYSCONV_EINVAL;
+    if (a->taps > 1 && a->slots > 0 && (a->state == nullptr || (a->slots > 1 && a->state_stride < (a->taps - 1) * a->channels)))
+        return SYSCONV_EINVAL;
+    if (a->x_stride < 0 || (a->rows > 1 && a->y_stride < a->channels)) return SYSCONV_EINVAL;
+    if (a->taps > 8 || a->channels > (1LL << 28)) return SYSCONV_EUNSUPPORTED;
+    int launches = 0;
+    return done(launch_causal_step(*a, static_cast<cudaStream_t>(stream), &launches), launches);
+}
+
+long long sysscan_saved_blocks(const sysscan_args *a)
+{
+    if (a == nullptr || check_sequences(a->seq) != SYSCONV_OK) return -1;
+    const sysconv_sequences &s = a->seq;
+    return s.offsets_dev ? s.total / kScanBlock + s.sequences : s.sequences * ((s.length + kScanBlock - 1) / kScanBlock);
+}
+
+long long sysscan_workspace_bytes(const sysscan_args *a) { return check_scan(a, false) == SYSCONV_OK ? scan_workspace(*a) : -1; }
+long long sysscan_backward_workspace_bytes(const sysscan_args *a)
+{
+    return check_scan(a, true) == SYSCONV_OK ? scan_backward_workspace(*a) : -1;
+}
+
+int sysscan(const sysscan_args *a, void *stream)
+{
+    const int st = check_scan(a, false);
+    if (st != SYSCONV_OK) return st;
+    if (!valid_workspace(a->workspace, a->workspace_bytes, scan_workspace(*a))) return SYSCONV_EINVAL;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int launches = 0;
+    switch (a->type) {
+        case SYSCONV_T_F32: return done(launch_scan_f32(*a, s, &launches), launches);
+        case SYSCONV_T_BF16: return done(launch_scan_bf16(*a, s, &launches), launches);
+        default: return done(launch_scan_f16(*a, s, &launches), launches);
+    }
+}
+
+int sysscan_backward(const sysscan_args *a, void *stream)
+{
+    const int st = check_scan(a, true);
+    if (st != SYSCONV_OK) return st;
+    if (!valid_workspace(a->workspace, a->workspace_bytes, scan_backward_workspace(*a))) return SYSCONV_EINVAL;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int launches = 0;
+    switch (a->type) {
+        case SYSCONV_T_F32: return done(launch_scan_backward_f32(*a, s, &launches), launches);
+        case SYSCONV_T_BF16: return done(launch_scan_backward_bf16(*a, s, &launches), launches);
+        default: return done(launch_scan_backward_f16(*a, s, &launches), launches);
+    }
+}
+
+int sysscan_step(const sysscan_step_args *a, void *stream)
+{
+    if (a == nullptr || a->rows < 1 || a->slots < 0 || a->channels < 1 || a->states < 1 || a->groups < 1 || a->channels % a->groups != 0 ||
+        !valid_type(a->type) || !a->u || !a->delta || !a->B || !a->C || !a->y || !a->A)
+        return SYSCONV_EINVAL;
+    if (a->slots > 0 && (a->state == nullptr || (a->slots > 1 && a->state_stride < a->channels * a->states))) return SYSCONV_EINVAL;
+    if (a->u_stride < 0 || a->delta_stride < 0 || a->z_stride < 0 || a->b_stride < 0 || a->c_stride < 0 ||
+        (a->rows > 1 && a->y_stride < a->channels))
+        return SYSCONV_EINVAL;
+    if (a->states > kMaxStates || a->channels > (1LL << 30) / a->states) return SYSCONV_EUNSUPPORTED;
+    int launches = 0;
+    return done(launch_scan_step(*a, static_cast<cudaStream_t>(stream), &launches), launches);
+}
+
+long long sysgroupnorm_workspace_bytes(const sysgroupnorm_args *a)
+{
+    return check_norm(a, false) == SYSCONV_OK ? groupnorm_workspace(*a) : -1;
+}
+long long sysgroupnorm_backward_workspace_bytes(const sysgroupnorm_args *a)
+{
+    return check_norm(a, true) == SYSCONV_OK ? groupnorm_backward_workspace(*a) : -1;
+}
+
+int sysgroupnorm(const sysgroupnorm_args *a, void *stream)
+{
+    const int st = check_norm(a, false);
+    if (st != SYSCONV_OK) return st;
+    if (!valid_workspace(a->workspace, a->workspace_bytes, groupnorm_workspace(*a))) return SYSCONV_EINVAL;
+    int launches = 0;
+    return done(launch_groupnorm(*a, static_cast<cudaStream_t>(stream), &launches), launches);
+}
+
+int sysgroupnorm_backward(const sysgroupnorm_args *a, void *stream)
+{
+    const int st = check_norm(a, true);
+    if (st != SYSCONV_OK) return st;
+    if (!valid_workspace(a->workspace, a->workspace_bytes, groupnorm_backward_workspace(*a))) return SYSCONV_EINVAL;
+    int launches = 0;
+    return done(launch_groupnorm_backward(*a, static_cast<cudaStream_t>(stream), &launches), launches);
+}
+
+}  // extern "C"

@@ -1,0 +1,540 @@
+// State space scan, backward.
+//
+// With dy' = dout silu(z) and g[t] = dL/dh[t] through y[t] and everything later:
+//   g[t]   = dy'[t] C[t] + a[t+1] g[t+1]                 a[t] = exp(d[t] A)
+//   dC[t]  = sum_c dy'[t] h[t]         dB[t] = sum_c g[t] d[t] u[t]
+//   p[t]   = g[t] a[t] h[t-1]          (gradient of d[t] A)          dA = sum_t p[t] d[t]
+//   r1[t]  = sum_n g[t] B[t]           r2[t] = sum_n p[t] A
+//   du     = d r1 + dy' D      dd = r2 + u r1      dz = dout (C.h + D u) silu'(z)
+//
+// Mapping as in the forward pass: states over LN lanes x S registers, a block marches along one sequence, here from its
+// last tile of 16 tokens to its first.  A tile starts from the state that the forward pass saved before it: h and a of
+// the 16 tokens are computed again into registers, then the tile is walked backwards.  Sums over the states (y, r1, r2)
+// are transposed over the LN lanes; sums over the channels (dB, dC) first over the warp's 32/LN channels by the same
+// halving exchange, then over the block's warps in shared memory, and leave as one partial row per block and token that
+// a second kernel adds up in a fixed order.  dA, dD and the bias gradient stay in registers over the march (per tile
+// first, so that long sums lose nothing) and are added over sequences at the end.
+//
+// Bound: issue slots and the fp32 pipe.  Per (token, channel, state): 2 x 3 packed operations forwards, 8 backwards, 1 exp,
+// and about 0.7 shuffles.
+#pragma once
+
+#include "state_scan.cuh"
+
+namespace sysconv {
+
+struct ScanBackArgs {
+    ScanArgs f;              // u, delta, z, B, C and the parameters; f.saved is read
+    Tokens dy, du, ddelta, dz, dB, dC;
+    float *bc_part;          // [channel block][flat token][lanes][2 S] partial sums of dB and dC
+    float *par_part;         // [sequence x chunk][channels x states + 2 channels] partial sums of dA, dD, ddelta_bias
+    const float *dfinal;
+    float *dstate, *dA, *dD, *ddbias;
+};
+
+template <int LN, int S>
+struct ScanBackShape {
+    static constexpr int NP = LN * S;
+    static constexpr int NT = LN <= 8 ? 128 : (NP >= 128 ? 256 : 16 * LN);   // threads: 16 channels a block where they fit
+    static constexpr int CB = NT / LN;
+    static constexpr int TB = kScanBlock;
+    static constexpr int U = LN < 16 ? LN : 16;
+    static constexpr int PP = TB * CB / NT > 0 ? TB * CB / NT : 1;
+    static constexpr int VT = PP >= 4 ? 4 : PP;
+    static constexpr int BE = TB * NP / NT > 0 ? TB * NP / NT : 1;
+    static constexpr int VB = BE >= 4 ? 4 : BE;
+    static constexpr int YP = CB + (LN < 32 ? 32 / LN : 1);
+    static constexpr int W = NT / 32;
+    static constexpr size_t bytes()
+    {
+        return sizeof(float) * (TB * CB * 4 + 2 * TB * NP + 3 * TB * YP + W * TB * 2 * NP);
+    }
+};
+
+template <typename T, int LN, int S>
+__global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kernel(ScanBackArgs b)
+{
+    using G = ScanBackShape<LN, S>;
+    constexpr int NP = G::NP, NT = G::NT, CB = G::CB, TB = G::TB, U = G::U, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB;
+    constexpr int YP = G::YP, W = G::W, P2 = S / 2, NV = 2 * S, CW = 32 / LN;
+    extern __shared__ __align__(16) float smem[];
+    float4 *s_p = reinterpret_cast<float4 *>(smem);                      // [TB][CB] d, d u, dy'
+    float *s_b = smem + TB * CB * 4;                                     // [TB][NP]
+    float *s_c = s_b + TB * NP;
+    float *s_y = s_c + TB * NP;                                          // [TB][YP] each: C.h, r1, r2
+    float *s_r1 = s_y + TB * YP, *s_r2 = s_r1 + TB * YP;
+    float *s_w = s_r2 + TB * YP;                                         // [W][TB][2 NP]
+    dependent_launch_enter();
+
+    const ScanArgs &a = b.f;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int grp = blockIdx.x / a.blocks_per_group;
+    const int c0 = grp * a.per_group + (blockIdx.x - grp * a.blocks_per_group) * CB;
+    const int c_end = min((grp + 1) * a.per_group, a.channels);
+    const int r = blockIdx.y;
+    const long long first = a.map.first(r), length = a.map.end(r) - first;
+    const long long t_begin = static_cast<long long>(blockIdx.z) * a.chunk;
+    const bool last_chunk = blockIdx.z + 1 == a.chunks || t_begin + a.chunk >= length;
+    const long long t_end = last_chunk ? length : t_begin + a.chunk;
+    const long long chain = static_cast<long long>(r) * a.chunks + blockIdx.z;
+
+    const int cl = tid / LN, ln = tid % LN, c = c0 + cl;
+    const bool own = c < c_end;
+    f32x2 A2[P2], carry[P2], dA[P2];
+    const bool empty = t_begin >= length && blockIdx.z > 0;              // its parameter sums are zero
+    {
+        float av[S], gv[S];
+        const float *from = a.chunks > 1 ? a.carry + chain * a.channels * a.states
+                                         : (b.dfinal ? b.dfinal + static_cast<long long>(r) * a.channels * a.states : nullptr);
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const int n = ln * S + i;
+            const long long at = static_cast<long long>(c) * a.states + n;
+            const bool ok = own && n < a.states;
+            av[i] = ok ? decay_rate(a.A[at]) : 0.0f;
+            gv[i] = ok && from && !empty ? from[at] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < P2; ++i) {
+            A2[i] = pair(av[2 * i], av[2 * i + 1]);
+            carry[i] = pair(gv[2 * i], gv[2 * i + 1]);
+            dA[i] = pair(0.0f, 0.0f);
+        }
+    }
+
+    const int pc = (tid * VT) % CB;
+    const T *B0 = token_row<T>(a.B, a.map, r, first) + grp * a.states;
+    const T *C0 = token_row<T>(a.C, a.map, r, first) + grp * a.states;
+    const T *u0 = token_row<T>(a.u, a.map, r, first) + c0 + pc;
+    const T *d0 = token_row<T>(a.delta, a.map, r, first) + c0 + pc;
+    const T *g0 = token_row<T>(b.dy, a.map, r, first) + c0 + pc;
+    const bool gate = a.z.ptr != nullptr;
+    const T *z0 = gate ? token_row<T>(a.z, a.map, r, first) + c0 + pc : nullptr;
+    T *du0 = token_row<T>(b.du, a.map, r, first) + c0 + pc;
+    T *dd0 = token_row<T>(b.ddelta, a.map, r, first) + c0 + pc;
+    T *dz0 = gate ? token_row<T>(b.dz, a.map, r, first) + c0 + pc : nullptr;
+    const int pvalid = c_end - c0 - pc;
+    float dbias[VT], dskip[VT], sum_d[VT], sum_b[VT];                    // parameters and their gradients, per channel
+#pragma unroll
+    for (int j = 0; j < VT; ++j) {
+        const bool ok = j < pvalid;
+        dbias[j] = ok && a.dbias ? a.dbias[c0 + pc + j] : 0.0f;
+        dskip[j] = ok && a.D ? a.D[c0 + pc + j] : 0.0f;
+        sum_d[j] = sum_b[j] = 0.0f;
+    }
+    const float *saved = a.saved + (saved_base(a.map, r, first) * a.channels + c) * a.states + ln * S;
+    float *part = b.bc_part + (static_cast<long long>(blockIdx.x) * a.map.total + first) * 2 * NP;
+
+    RawTok<T, PP, VT> ru, rd, rz, rg;
+    RawTok<T, BE, VB> rb, rc;
+    float rh[S];
+    auto fetch = [&](long long t0) {
+#pragma unroll
+        for (int i = 0; i < PP / VT; ++i) {
+            const int e = (i * NT + tid) * VT;
+            const long long t = t0 + e / CB;
+            const int valid = e < TB * CB && t < t_end ? pvalid : 0;
+            ru.v[i] = load_some<T, VT>(u0 + t * a.u.tstride, valid, a.wide_tok);
+            rd.v[i] = load_some<T, VT>(d0 + t * a.delta.tstride, valid, a.wide_tok);
+            rg.v[i] = load_some<T, VT>(g0 + t * b.dy.tstride, valid, a.wide_tok);
+            if (gate) rz.v[i] = load_some<T, VT>(z0 + t * a.z.tstride, valid, a.wide_tok);
+        }
+#pragma unroll
+        for (int i = 0; i < BE / VB; ++i) {
+            const int e = (i * NT + tid) * VB;
+            const long long t = t0 + e / NP;
+            const int n = e % NP;
+            const int valid = e < TB * NP && t < t_end ? a.states - n : 0;
+            rb.v[i] = load_some<T, VB>(B0 + t * a.B.tstride + n, valid, a.wide_bc);
+            rc.v[i] = load_some<T, VB>(C0 + t * a.C.tstride + n, valid, a.wide_bc);
+        }
+        const float *from = saved + t0 / kScanBlock * a.channels * a.states;
+#pragma unroll
+        for (int i = 0; i < S; ++i) rh[i] = own && ln * S + i < a.states ? from[i] : 0.0f;
+    };
+
+    const long long tiles = empty || t_end <= t_begin ? 0 : (t_end - t_begin + TB - 1) / TB;
+    if (tiles > 0) fetch(t_begin + (tiles - 1) * TB);
+    for (long long tile = tiles - 1; tile >= 0; --tile) {
+        const long long t0 = t_begin + tile * TB;
+        float uv[PP], dv[PP], slope[PP], dyv[PP], zf[PP];
+#pragma unroll
+        for (int i = 0; i < PP / VT; ++i) {
+            const int e = (i * NT + tid) * VT;
+            if (e < TB * CB) {
+                const int tt = e / CB;
+                const bool live = t0 + tt < t_end;
+#pragma unroll
+                for (int j = 0; j < VT; ++j) {
+                    const int q = i * VT + j;
+                    const float raw = to_f32(rd.v[i].v[j]) + dbias[j], dout = to_f32(rg.v[i].v[j]);
+                    uv[q] = to_f32(ru.v[i].v[j]);
+                    dv[q] = live ? (a.softplus ? softplus(raw) : raw) : 0.0f;
+                    slope[q] = a.softplus ? sigmoid(raw) : 1.0f;
+                    if (gate) {
+                        const float z = to_f32(rz.v[i].v[j]), sig = sigmoid(z);
+                        dyv[q] = dout * z * sig;
+                        zf[q] = dout * silu_slope(z, sig);
+                    } else {
+                        dyv[q] = dout;
+                    }
+                    s_p[tt * CB + pc + j] = make_float4(dv[q], dv[q] * uv[q], dyv[q], 0.0f);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BE / VB; ++i) {
+            const int e = (i * NT + tid) * VB;
+            if (e < TB * NP) {
+#pragma unroll
+                for (int j = 0; j < VB; ++j) {
+                    s_b[e + j] = to_f32(rb.v[i].v[j]);
+                    s_c[e + j] = to_f32(rc.v[i].v[j]);
+                }
+            }
+        }
+        f32x2 h[TB + 1][P2], dec[TB][P2];
+#pragma unroll
+        for (int i = 0; i < P2; ++i) h[0][i] = pair(rh[2 * i], rh[2 * i + 1]);
+        __syncthreads();
+        if (tile > 0) fetch(t0 - TB);
+
+        // forwards: states and decays of the tile, y
+#pragma unroll
+        for (int tu = 0; tu < TB; tu += U) {
+            float sums[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int t = tu + k;
+                const float2 d = *reinterpret_cast<const float2 *>(&s_p[t * CB + cl]);
+                f32x2 acc;
+#pragma unroll
+                for (int i = 0; i < P2; ++i) {
+                    const float2 bv = *reinterpret_cast<const float2 *>(&s_b[t * NP + ln * S + 2 * i]);
+                    const float2 cv = *reinterpret_cast<const float2 *>(&s_c[t * NP + ln * S + 2 * i]);
+                    const float2 x = halves(mul2(A2[i], pair(d.x, d.x)));
+                    dec[t][i] = pair(exp2_fast(x.x), exp2_fast(x.y));
+                    h[t + 1][i] = fma2(dec[t][i], h[t][i], mul2(pair(bv.x, bv.y), pair(d.y, d.y)));
+                    acc = i == 0 ? mul2(h[t + 1][i], pair(cv.x, cv.y)) : fma2(h[t + 1][i], pair(cv.x, cv.y), acc);
+                }
+                const float2 v = halves(acc);
+                sums[k] = v.x + v.y;
+            }
+            if (gate) {
+                const float v = sum_transposed<U, LN>(sums, lane);
+                if (LN <= U || ln < U) s_y[(tu + ln % U) * YP + cl] = v;
+            }
+        }
+        // backwards
+        f32x2 dA_tile[P2];
+#pragma unroll
+        for (int i = 0; i < P2; ++i) dA_tile[i] = pair(0.0f, 0.0f);
+#pragma unroll
+        for (int tu = TB - U; tu >= 0; tu -= U) {
+            float sums1[U], sums2[U];
+#pragma unroll
+            for (int k = U - 1; k >= 0; --k) {
+                const int t = tu + k;
+                const float4 p = s_p[t * CB + cl];
+                f32x2 acc1, acc2;
+                float v[NV];
+#pragma unroll
+                for (int i = 0; i < P2; ++i) {
+                    const float2 bv = *reinterpret_cast<const float2 *>(&s_b[t * NP + ln * S + 2 * i]);
+                    const float2 cv = *reinterpret_cast<const float2 *>(&s_c[t * NP + ln * S + 2 * i]);
+                    const f32x2 g = fma2(pair(p.z, p.z), pair(cv.x, cv.y), carry[i]);
+                    const float2 db = halves(mul2(g, pair(p.y, p.y))), dc = halves(mul2(h[t + 1][i], pair(p.z, p.z)));
+                    v[2 * i] = db.x;
+                    v[2 * i + 1] = db.y;
+                    v[S + 2 * i] = dc.x;
+                    v[S + 2 * i + 1] = dc.y;
+                    carry[i] = mul2(g, dec[t][i]);
+                    const f32x2 dlog = mul2(carry[i], h[t][i]);
+                    dA_tile[i] = fma2(dlog, pair(p.x, p.x), dA_tile[i]);
+                    acc1 = i == 0 ? mul2(g, pair(bv.x, bv.y)) : fma2(g, pair(bv.x, bv.y), acc1);
+                    acc2 = i == 0 ? mul2(dlog, A2[i]) : fma2(dlog, A2[i], acc2);
+                }
+                const float2 w1 = halves(acc1), w2 = halves(acc2);
+                sums1[k] = w1.x + w1.y;
+                sums2[k] = w2.x + w2.y;
+                // over the warp's channels: lanes that differ above the LN bits
+                int at = 0, nv = NV;
+                bool writes = true;
+#pragma unroll
+                for (int w = 16; w >= LN; w /= 2) {
+                    const bool up = lane & w;
+                    if (nv > 1) {
+                        nv /= 2;
+#pragma unroll
+                        for (int i = 0; i < nv; ++i) {
+                            const float give = up ? v[i] : v[i + nv];
+                            const float keep = up ? v[i + nv] : v[i];
+                            v[i] = keep + __shfl_xor_sync(kFullMask, give, w);
+                        }
+                        at += up ? nv : 0;
+                    } else {
+                        v[0] += __shfl_xor_sync(kFullMask, v[0], w);
+                        writes = writes && !up;
+                    }
+                }
+                constexpr int LEFT = NV > CW ? NV / CW : 1;
+                float *to = s_w + (warp * TB + t) * 2 * NP + ln * NV + at;
+                if (writes)
+#pragma unroll
+                    for (int i = 0; i < LEFT; ++i) to[i] = v[i];
+            }
+            const float v1 = sum_transposed<U, LN>(sums1, lane), v2 = sum_transposed<U, LN>(sums2, lane);
+            if (LN <= U || ln < U) {
+                s_r1[(tu + ln % U) * YP + cl] = v1;
+                s_r2[(tu + ln % U) * YP + cl] = v2;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < P2; ++i) dA[i] = fma2(dA_tile[i], pair(1.0f, 1.0f), dA[i]);
+        __syncthreads();
+
+#pragma unroll
+        for (int i = 0; i < PP / VT; ++i) {
+            const int e = (i * NT + tid) * VT;
+            const int tt = e / CB;
+            if (e < TB * CB && t0 + tt < t_end) {
+                Pack<T, VT> odu, odd, odz;
+#pragma unroll
+                for (int j = 0; j < VT; ++j) {
+                    const int q = i * VT + j, at = tt * YP + pc + j;
+                    const float r1 = s_r1[at], r2 = s_r2[at] * 0.69314718055994531f;      // A2 is A log2(e)
+                    const float dd = fmaf(uv[q], r1, r2) * slope[q];
+                    odu.v[j] = from_f32<T>(fmaf(dv[q], r1, dyv[q] * dskip[j]));
+                    odd.v[j] = from_f32<T>(dd);
+                    if (gate) odz.v[j] = from_f32<T>(fmaf(dskip[j], uv[q], s_y[at]) * zf[q]);
+                    sum_b[j] += dd;
+                    sum_d[j] = fmaf(dyv[q], uv[q], sum_d[j]);
+                }
+                store_some<T, VT>(du0 + (t0 + tt) * b.du.tstride, odu, pvalid, a.wide_tok);
+                store_some<T, VT>(dd0 + (t0 + tt) * b.ddelta.tstride, odd, pvalid, a.wide_tok);
+                if (gate) store_some<T, VT>(dz0 + (t0 + tt) * b.dz.tstride, odz, pvalid, a.wide_tok);
+            }
+        }
+        for (int e = tid; e < TB * 2 * NP; e += NT) {
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) v += s_w[w * TB * 2 * NP + e];
+            if (t0 + e / (2 * NP) < t_end) part[t0 * 2 * NP + e] = v;
+        }
+    }
+
+    if (b.dstate != nullptr && blockIdx.z == 0 && own) {
+        float *to = b.dstate + (static_cast<long long>(r) * a.channels + c) * a.states;
+#pragma unroll
+        for (int i = 0; i < P2; ++i) {
+            const float2 v = halves(carry[i]);
+            if (ln * S + 2 * i < a.states) to[ln * S + 2 * i] = v.x;
+            if (ln * S + 2 * i + 1 < a.states) to[ln * S + 2 * i + 1] = v.y;
+        }
+    }
+    float *row = b.par_part + chain * (static_cast<long long>(a.channels) * (a.states + 2));
+    if (own) {
+        float *to = row + static_cast<long long>(c) * a.states;
+#pragma unroll
+        for (int i = 0; i < P2; ++i) {
+            const float2 v = halves(dA[i]);
+            if (ln * S + 2 * i < a.states) to[ln * S + 2 * i] = v.x;
+            if (ln * S + 2 * i + 1 < a.states) to[ln * S + 2 * i + 1] = v.y;
+        }
+    }
+    __syncthreads();
+    float *sum = smem;                                                   // [threads][2 VT]
+#pragma unroll
+    for (int j = 0; j < VT; ++j) {
+        sum[tid * 2 * VT + j] = sum_d[j];
+        sum[tid * 2 * VT + VT + j] = sum_b[j];
+    }
+    __syncthreads();
+    for (int q = tid; q < 2 * CB; q += NT) {
+        const int which = q / CB, ch = q % CB, j = ch % VT;
+        if (c0 + ch < c_end) {
+            float v = 0.0f;
+            for (int w = ch / VT; w < NT; w += CB / VT) v += sum[w * 2 * VT + which * VT + j];
+            row[static_cast<long long>(a.channels) * (a.states + which) + c0 + ch] = v;
+        }
+    }
+}
+
+// Chains the chunks' carries from the last to the first: what each chunk receives from the tokens behind it.
+static __global__ void scan_chain_back_kernel(ScanBackArgs b)
+{
+    dependent_launch_enter();
+    const ScanArgs &a = b.f;
+    const long long id = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
+    const int cn = a.channels * a.states;
+    const int r = static_cast<int>(id / cn);
+    if (r >= a.map.sequences) return;
+    const int e = static_cast<int>(id - static_cast<long long>(r) * cn), c = e / a.states;
+    const long long length = a.map.end(r) - a.map.first(r);
+    float carry = b.dfinal ? b.dfinal[id] : 0.0f;
+    const float A = decay_rate(a.A[e]);
+    const long long used = length <= 0 ? 1 : min(static_cast<long long>(a.chunks), (length + a.chunk - 1) / a.chunk);
+    for (long long k = used - 1; k >= 0; --k) {
+        const long long chain = static_cast<long long>(r) * a.chunks + k;
+        const float local = k > 0 ? a.carry[chain * cn + e] : 0.0f, sum = k > 0 ? a.dsum[chain * a.channels + c] : 0.0f;
+        a.carry[chain * cn + e] = carry;
+        carry = fmaf(exp2_fast(A * sum), carry, local);
+    }
+}
+
+// dB and dC: the partial rows of a group's channel blocks, added in order.  One thread per (token, group, lane, value).
+template <typename T, int LN, int S>
+__global__ void __launch_bounds__(256) scan_bc_kernel(ScanBackArgs b)
+{
+    constexpr int NP2 = 2 * LN * S;
+    dependent_launch_enter();
+    const ScanArgs &a = b.f;
+    const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const int p = static_cast<int>(id % NP2);
+    const long long tg = id / NP2;
+    const long long flat = tg / a.groups;
+    const int grp = static_cast<int>(tg - flat * a.groups);
+    if (flat >= a.map.total) return;
+    const int k = p % (2 * S), n = p / (2 * S) * S + k % S;
+    if (n >= a.states) return;
+    const int r = a.map.find(flat);
+    if (flat < a.map.first(r) || flat >= a.map.end(r)) return;           // a token of no sequence
+    const float *from = b.bc_part + (static_cast<long long>(grp) * a.blocks_per_group * a.map.total + flat) * NP2 + p;
+    const long long step = a.map.total * NP2;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < a.blocks_per_group; ++i) v += from[i * step];
+    T *to = token_row<T>(k < S ? b.dB : b.dC, a.map, r, flat) + grp * a.states + n;
+    *to = from_f32<T>(v);
+}
+
+// dA, dD, ddelta_bias: column sums of par_part over sequences and chunks.
+static __global__ void __launch_bounds__(256) scan_param_kernel(ScanBackArgs b)
+{
+    dependent_launch_enter();
+    const ScanArgs &a = b.f;
+    const long long columns = static_cast<long long>(a.channels) * (a.states + 2);
+    const long long col = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (col >= columns) return;
+    const long long rows = static_cast<long long>(a.map.sequences) * a.chunks;
+    float v = 0.0f;
+#pragma unroll 4
+    for (long long i = 0; i < rows; ++i) v += b.par_part[i * columns + col];
+    const long long cn = static_cast<long long>(a.channels) * a.states;
+    if (col < cn) {
+        if (b.dA) b.dA[col] = v;
+    } else if (col < cn + a.channels) {
+        if (b.dD) b.dD[col - cn] = v;
+    } else if (b.ddbias) {
+        b.ddbias[col - cn - a.channels] = v;
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------
+
+struct ScanBackPlan {
+    int ln, s, chunk, chunks;
+    long long bc_floats, par_floats, carry_floats, dsum_floats;
+};
+ScanBackPlan scan_backward_plan(const sysscan_args &a);
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_kernel_smem(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t bytes, cudaStream_t s, Args &&...args)
+{
+    if (bytes > 48 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+        if (err != cudaSuccess) return err;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent_launch_enabled() ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
+template <typename T, int LN, int S>
+cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *launches)
+{
+    using G = ScanBackShape<LN, S>;
+    const int per_group = b.f.per_group;
+    cudaError_t err;
+    if (b.f.chunks > 1) {
+        using F = ScanShape<LN, S>;
+        ScanArgs k = b.f;
+        k.u = b.dy;
+        k.B = b.f.C;
+        k.blocks_per_group = ceil_div(per_group, F::CB);
+        err = launch_kernel(scan_kernel<T, LN, S, kChunkBack>, dim3(k.blocks_per_group * k.groups, k.map.sequences, k.chunks),
+                            dim3(kScanThreads), s, k);
+        if (err != cudaSuccess) return err;
+        const long long n = static_cast<long long>(k.map.sequences) * k.channels * k.states;
+        err = launch_kernel(scan_chain_back_kernel, dim3(ceil_div(n, 256)), dim3(256), s, b);
+        if (err != cudaSuccess) return err;
+        *launches += 2;
+    }
+    b.f.blocks_per_group = ceil_div(per_group, G::CB);
+    err = launch_kernel_smem(scan_backward_kernel<T, LN, S>, dim3(b.f.blocks_per_group * b.f.groups, b.f.map.sequences, b.f.chunks),
+                             dim3(G::NT), G::bytes(), s, b);
+    if (err != cudaSuccess) return err;
+    *launches += 1;
+    const long long values = b.f.map.total * b.f.groups * 2 * LN * S;
+    if (values > 0) {
+        err = launch_kernel(scan_bc_kernel<T, LN, S>, dim3(ceil_div(values, 256)), dim3(256), s, b);
+        if (err != cudaSuccess) return err;
+        *launches += 1;
+    }
+    *launches += 1;
+    return launch_kernel(scan_param_kernel, dim3(ceil_div(static_cast<long long>(b.f.channels) * (b.f.states + 2), 256)), dim3(256), s, b);
+}
+
+template <typename T>
+cudaError_t launch_scan_backward_t(const sysscan_args &a, cudaStream_t s, int *launches)
+{
+    const ScanBackPlan p = scan_backward_plan(a);
+    const size_t esz = sizeof(T);
+    ScanPlan fp = {};
+    fp.ln = p.ln;
+    fp.s = p.s;
+    fp.chunk = p.chunk;
+    fp.chunks = p.chunks;
+    fp.carry_floats = p.carry_floats;
+    sysscan_args f = a;
+    f.y = a.dy;                                                          // the arrays whose alignment counts here
+    f.state = nullptr;
+    f.final_state = nullptr;
+    ScanBackArgs b = {};
+    b.f = scan_args(f, fp);
+    b.f.y = Tokens{};
+    b.f.wide_tok = b.f.wide_tok && scan_rows_wide(a, a.du, esz) && scan_rows_wide(a, a.ddelta, esz) && scan_rows_wide(a, a.dz, esz);
+    b.dy = make_tokens(a.dy);
+    b.du = make_tokens(a.du);
+    b.ddelta = make_tokens(a.ddelta);
+    b.dz = make_tokens(a.dz);
+    b.dB = make_tokens(a.dB);
+    b.dC = make_tokens(a.dC);
+    b.dfinal = static_cast<const float *>(a.dfinal);
+    b.dstate = static_cast<float *>(a.dstate);
+    b.dA = static_cast<float *>(a.dA);
+    b.dD = static_cast<float *>(a.dD);
+    b.ddbias = static_cast<float *>(a.ddelta_bias);
+    b.bc_part = b.f.carry + p.carry_floats + p.dsum_floats;
+    b.par_part = b.bc_part + p.bc_floats;
+    switch (p.ln * 8 + p.s) {
+        case 1 * 8 + 2: return launch_scan_backward_shape<T, 1, 2>(b, s, launches);
+        case 2 * 8 + 2: return launch_scan_backward_shape<T, 2, 2>(b, s, launches);
+        case 4 * 8 + 2: return launch_scan_backward_shape<T, 4, 2>(b, s, launches);
+        case 8 * 8 + 2: return launch_scan_backward_shape<T, 8, 2>(b, s, launches);
+        case 16 * 8 + 2: return launch_scan_backward_shape<T, 16, 2>(b, s, launches);
+        case 32 * 8 + 2: return launch_scan_backward_shape<T, 32, 2>(b, s, launches);
+        case 32 * 8 + 4: return launch_scan_backward_shape<T, 32, 4>(b, s, launches);
+        default: return kNoInstantiation;
+    }
+}
+
+}  // namespace sysconv

@@ -53,6 +53,19 @@ const DeviceInfo *device_info()
 inline size_t in_elt_bytes(int dtype) { return dtype == SYSCONV_F32 ? 4 : 1; }
 inline long long align256(long long v) { return (v + 255) & ~255LL; }
 
+}  // namespace
+
+namespace sysconv {
+void count_launches(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
+int device_sm_count()
+{
+    const DeviceInfo *d = device_info();
+    return d ? d->sm_count : 0;
+}
+}  // namespace sysconv
+
+namespace {
+
 // a * b * c for positive factors, or -1 if the product (plus alignment slack) would not fit a long long
 long long checked_product(long long a, long long b, long long c)
 {
