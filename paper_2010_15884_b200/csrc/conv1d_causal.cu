@@ -13,21 +13,6 @@ namespace {
 
 constexpr int kThreads = 128;
 
-template <typename T, int V>
-__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&f)[V])
-{
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f32(p.v[i]);
-}
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> pack(const float (&f)[V])
-{
-    Pack<T, V> p;
-#pragma unroll
-    for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(f[i]);
-    return p;
-}
-
 template <typename T>
 __device__ __forceinline__ float load_param(const void *p, long long i, bool f32)
 {
@@ -99,7 +84,7 @@ template <typename T, int V, int K>
 __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
 {
     dependent_launch_enter();
-    constexpr int U = 4;                                            // tokens in flight per thread
+    constexpr int U = 8;                                            // tokens in flight per thread
     const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     const long long run = id / a.groups;
     if (run >= a.runs) return;
@@ -122,35 +107,30 @@ __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
         load_window<T, V, K>(a, r, first, t, c, win);
         const T *src = token_row<T>(a.x, a.map, r, t) + c;
         T *dst = token_row<T>(a.y, a.map, r, t) + c;
-        while (t < last) {
-            const int n = static_cast<int>(min(last - t, static_cast<long long>(U)));
+        auto step = [&](const Pack<T, V> &raw, T *to) {
+            unpack(raw, win[K - 1]);
+            float out[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float v = bias[i];
+#pragma unroll
+                for (int k = 0; k < K; ++k) v = fmaf(w[k][i], win[k][i], v);
+                out[i] = a.silu ? silu(v) : v;
+            }
+            store_pack(to, pack<T, V>(out));
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
+        };
+        for (; t + U <= last; t += U, src += U * a.x.tstride, dst += U * a.y.tstride) {
             Pack<T, V> raw[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (u < n) raw[u] = load_pack<T, V>(src + u * a.x.tstride);
+            for (int u = 0; u < U; ++u) raw[u] = load_pack<T, V>(src + u * a.x.tstride);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (u < n) {
-                    unpack(raw[u], win[K - 1]);
-                    float out[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        float v = bias[i];
-#pragma unroll
-                        for (int k = 0; k < K; ++k) v = fmaf(w[k][i], win[k][i], v);
-                        out[i] = a.silu ? silu(v) : v;
-                    }
-                    store_pack(dst + u * a.y.tstride, pack<T, V>(out));
-#pragma unroll
-                    for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
-                }
-            }
-            t += n;
-            src += n * a.x.tstride;
-            dst += n * a.y.tstride;
+            for (int u = 0; u < U; ++u) step(raw[u], dst + u * a.y.tstride);
         }
+        for (; t < last; ++t, src += a.x.tstride, dst += a.y.tstride) step(load_pack<T, V>(src), dst);
         if (t >= end) {                                             // (t > end: descending offsets; never loop on them)
             store_state<T, V, K>(a, r, c, win);
             r = pass_empty<T, V, K>(a, r + 1, t, c);
@@ -377,7 +357,7 @@ __global__ void __launch_bounds__(kThreads) causal_step_kernel(CausalStepArgs a)
         float v = a.bias ? load_param<T>(a.bias, c + i, a.weight_f32) : 0.0f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            v = fmaf(load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32), to_f32(line[k].v[i]), v);
+            v = fmaf(load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32), line[k].get(i), v);
         out[i] = a.silu ? silu(v) : v;
     }
     store_pack(dst, pack<T, V>(out));
@@ -404,9 +384,7 @@ cudaError_t with_taps(long long k, F f)
     }
 }
 
-// channels per thread of the 128-bit form; fewer for long filters, whose windows would not fit the registers
-template <typename T, int K>
-constexpr int wide_forward() { return sizeof(T) == 2 && K <= 4 ? 8 : 4; }
+constexpr int kWide = 4;                 // channels per thread of the aligned forms
 
 CausalArgs base_args(const sysconv_causal_args &a)
 {
@@ -467,7 +445,7 @@ cudaError_t launch_causal(const sysconv_causal_args &a, cudaStream_t s, int *lau
         using T = std::remove_pointer_t<decltype(tag)>;
         return with_taps(a.taps, [&](auto taps) {
             constexpr int K = decltype(taps)::value;
-            constexpr int V = wide_forward<T, K>();
+            constexpr int V = kWide;
             const bool packed = a.seq.offsets_dev != nullptr;
             const size_t bytes = V * sizeof(T);
             const bool wide = rows_aligned(a.x, packed, sizeof(T), bytes) && rows_aligned(a.y, packed, sizeof(T), bytes) &&

@@ -97,8 +97,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                x[i][j] = to_f32(raw[i].v[j]);
-                if (BACK) e[i][j] = to_f32(rdy[i].v[j]);
+                x[i][j] = raw[i].get(j);
+                if (BACK) e[i][j] = rdy[i].get(j);
             }
         const float shift = __shfl_sync(kFullMask, x[0][0], 0);
         if (b + a.entry_step < a.batch) fetch(b + a.entry_step);
@@ -123,13 +123,13 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
 #pragma unroll
             for (int i = 0; i < R; ++i)
                 if (lane + 32 * i < count) {
-                    Pack<T, V> out;
+                    float out[V];
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float v = fmaf((x[i][j] - mean) * rstd, wv[i][j], bv[i][j]);
-                        out.v[j] = from_f32<T>(a.silu ? silu(v) : v);
+                        out[j] = a.silu ? silu(v) : v;
                     }
-                    store_pack(norm_at<T>(a.y, b, at_s[i], at_c[i]), out);
+                    store_pack(norm_at<T>(a.y, b, at_s[i], at_c[i]), pack<T, V>(out));
                 }
         } else {
             const float mean = a.mean[b * a.groups + g], rstd = a.rstd[b * a.groups + g];
@@ -157,11 +157,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
 #pragma unroll
             for (int i = 0; i < R; ++i)
                 if (lane + 32 * i < count) {
-                    Pack<T, V> out;
+                    float out[V];
 #pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        out.v[j] = from_f32<T>(rstd * (fmaf(e[i][j], wv[i][j], -s.x) - x[i][j] * s.y));
-                    store_pack(norm_at<T>(a.dx, b, at_s[i], at_c[i]), out);
+                    for (int j = 0; j < V; ++j) out[j] = rstd * (fmaf(e[i][j], wv[i][j], -s.x) - x[i][j] * s.y);
+                    store_pack(norm_at<T>(a.dx, b, at_s[i], at_c[i]), pack<T, V>(out));
                 }
         }
     }
@@ -229,7 +228,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs a)
                 for (int u = 0; u < UN; ++u)
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float v = to_f32(raw[u].v[j]) - shift;
+                        const float v = raw[u].get(j) - shift;
                         s.x += v;
                         s.y = fmaf(v, v, s.y);
                     }
@@ -238,7 +237,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs a)
                 const Pack<T, V> raw = load_pack<T, V>(src);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float v = to_f32(raw.v[j]) - shift;
+                    const float v = raw.get(j) - shift;
                     s.x += v;
                     s.y = fmaf(v, v, s.y);
                 }
@@ -311,20 +310,20 @@ __global__ void __launch_bounds__(kNormThreads) norm_apply_kernel(NormArgs a)
             bias[j] = a.b ? a.b[c + j] : 0.0f;
         }
         auto one = [&](const Pack<T, V> &x, const Pack<T, V> &dy) {
-            Pack<T, V> out;
+            float out[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float xh = (to_f32(x.v[j]) - mean) * rstd;
+                const float xh = (x.get(j) - mean) * rstd;
                 const float v = fmaf(xh, w[j], bias[j]);
                 if (BACK) {
-                    float e = to_f32(dy.v[j]);
+                    float e = dy.get(j);
                     if (a.silu) e *= silu_slope(v, sigmoid(v));
-                    out.v[j] = from_f32<T>(rstd * (fmaf(e, w[j], -m1) - xh * m2));
+                    out[j] = rstd * (fmaf(e, w[j], -m1) - xh * m2);
                 } else {
-                    out.v[j] = from_f32<T>(a.silu ? silu(v) : v);
+                    out[j] = a.silu ? silu(v) : v;
                 }
             }
-            return out;
+            return pack<T, V>(out);
         };
         long long row = p.row0 + p.r0;
         const Tokens &to = BACK ? a.dx : a.y;
@@ -377,8 +376,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_stats_kernel(NormArgs 
             auto add = [&](const Pack<T, V> &x, const Pack<T, V> &dy) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float xh = (to_f32(x.v[j]) - mean) * rstd;
-                    float e = to_f32(dy.v[j]);
+                    const float xh = (x.get(j) - mean) * rstd;
+                    float e = dy.get(j);
                     if (a.silu) {
                         const float v = fmaf(xh, w[j], bias[j]);
                         e *= silu_slope(v, sigmoid(v));
@@ -423,37 +422,84 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_stats_kernel(NormArgs 
     }
 }
 
-// Joins the slabs of one (batch entry, group): per channel sums for dw and db, and the group's means of p and p xhat.
-__global__ void __launch_bounds__(128) norm_back_join_kernel(NormArgs a)
+// Joins the slabs of one batch entry and a few groups: per channel sums for dw and db, and the groups' means of p and
+// p xhat.  The block's threads are channels x slab lanes.
+constexpr int kJoinChannels = 64;        // channels per block, unless one group has more
+
+__global__ void __launch_bounds__(kNormThreads) norm_back_join_kernel(NormArgs a)
 {
     dependent_launch_enter();
-    __shared__ float2 sums[4];
+    __shared__ float2 sums[kNormThreads], group[kNormThreads / 32];
     const long long b = blockIdx.y;
-    const int g = blockIdx.x;
-    float2 t = make_float2(0.0f, 0.0f);
-    for (int i = threadIdx.x; i < a.cg; i += 128) {
-        const int c = g * a.cg + i;
-        const float *from = a.part + b * a.slabs * 2 * a.channels + c;
+    const int per = a.cg >= kJoinChannels ? 1 : kJoinChannels / a.cg;    // groups per block
+    const int g0 = blockIdx.x * per, ng = min(per, a.groups - g0);
+    const int n = ng * a.cg, width = min(n, kNormThreads), lanes = kNormThreads / width;
+    const int ch = threadIdx.x % width, sl = threadIdx.x / width;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float2 wide = make_float2(0.0f, 0.0f);                               // one wide group: this thread's part of its sums
+    for (int i = ch; i < (n + width - 1) / width * width; i += width) {
+        const int c = g0 * a.cg + i;
         float s1 = 0.0f, s2 = 0.0f;
+        if (i < n && sl < lanes) {
+            const float *from = a.part + b * a.slabs * 2 * a.channels + c;
 #pragma unroll 4
-        for (int k = 0; k < a.slabs; ++k) {
-            s1 += from[static_cast<long long>(k) * 2 * a.channels];
-            s2 += from[static_cast<long long>(k) * 2 * a.channels + a.channels];
+            for (int k = sl; k < a.slabs; k += lanes) {
+                s1 += from[static_cast<long long>(k) * 2 * a.channels];
+                s2 += from[static_cast<long long>(k) * 2 * a.channels + a.channels];
+            }
         }
-        a.pq[b * 2 * a.channels + c] = s1;
-        a.pq[(b * 2 + 1) * a.channels + c] = s2;
-        const float w = a.w ? a.w[c] : 1.0f;
-        t.x = fmaf(w, s1, t.x);
-        t.y = fmaf(w, s2, t.y);
+        if (lanes > 1) {
+            __syncthreads();
+            sums[threadIdx.x] = make_float2(s1, s2);
+            __syncthreads();
+            if (sl == 0)
+                for (int k = 1; k < lanes; ++k) {
+                    s1 += sums[k * width + ch].x;
+                    s2 += sums[k * width + ch].y;
+                }
+        }
+        float2 p = make_float2(0.0f, 0.0f);
+        if (i < n && sl == 0) {
+            a.pq[b * 2 * a.channels + c] = s1;
+            a.pq[(b * 2 + 1) * a.channels + c] = s2;
+            const float w = a.w ? a.w[c] : 1.0f;
+            p = make_float2(w * s1, w * s2);
+        }
+        wide.x += p.x;
+        wide.y += p.y;
     }
-    t = warp_sum(t);
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = t;
+    const float inv = 1.0f / (static_cast<float>(a.space) * static_cast<float>(a.cg));
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const float inv = 1.0f / (static_cast<float>(a.space) * static_cast<float>(a.cg));
-        float *to = a.group_sums + 2 * (b * a.groups + g);
-        to[0] = (sums[0].x + sums[1].x + sums[2].x + sums[3].x) * inv;
-        to[1] = (sums[0].y + sums[1].y + sums[2].y + sums[3].y) * inv;
+    sums[threadIdx.x] = wide;
+    __syncthreads();
+    if (ng == 1) {
+        const float2 t = warp_sum(sums[threadIdx.x]);
+        if (lane == 0) group[warp] = t;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float2 v = group[0];
+            for (int k = 1; k < kNormThreads / 32; ++k) {
+                v.x += group[k].x;
+                v.y += group[k].y;
+            }
+            float *to = a.group_sums + 2 * (b * a.groups + g0);
+            to[0] = v.x * inv;
+            to[1] = v.y * inv;
+        }
+        return;
+    }
+    for (int g = warp; g < ng; g += kNormThreads / 32) {                 // several groups: width is all their channels
+        float2 t = make_float2(0.0f, 0.0f);
+        for (int i = lane; i < a.cg; i += 32) {
+            t.x += sums[g * a.cg + i].x;
+            t.y += sums[g * a.cg + i].y;
+        }
+        t = warp_sum(t);
+        if (lane == 0) {
+            float *to = a.group_sums + 2 * (b * a.groups + g0 + g);
+            to[0] = t.x * inv;
+            to[1] = t.y * inv;
+        }
     }
 }
 
@@ -673,7 +719,8 @@ cudaError_t launch_groupnorm_backward(const sysgroupnorm_args &a, cudaStream_t s
                 const dim3 grid(p.slabs, p.tiles, static_cast<unsigned>(q.batch)), block(kNormThreads);
                 cudaError_t e = launch_kernel(norm_back_stats_kernel<T, V>, grid, block, s, q);
                 if (e == cudaSuccess)
-                    e = launch_kernel(norm_back_join_kernel, dim3(q.groups, static_cast<unsigned>(q.batch)), dim3(128), s, q);
+                    e = launch_kernel(norm_back_join_kernel, dim3(ceil_div(q.groups, q.cg >= kJoinChannels ? 1 : kJoinChannels / q.cg), static_cast<unsigned>(q.batch)),
+                                      dim3(kNormThreads), s, q);
                 if (e == cudaSuccess) e = launch_kernel(norm_apply_kernel<T, V, true>, grid, block, s, q);
                 *launches += 3;
                 return e;

@@ -20,21 +20,134 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// V consecutive elements that move as one aligned access (V * sizeof(T) is 2, 4, 8 or 16 bytes, or 32 as two)
+// V consecutive elements that move as one aligned access, kept as the 32-bit words they were loaded as and converted only
+// when they are used (taking them apart at once would wait for the load).
 template <typename T, int V>
-struct alignas(sizeof(T) * V > 16 ? 16 : sizeof(T) * V) Pack {
-    T v[V];
+struct Pack {
+    static constexpr int W = (V * static_cast<int>(sizeof(T)) + 3) / 4;
+    uint32_t w[W];
+    __device__ __forceinline__ float get(int i) const;
 };
+template <typename T> struct Bits;
+template <> struct Bits<float> {
+    static __device__ __forceinline__ float get(const uint32_t *w, int i) { return __uint_as_float(w[i]); }
+    static __device__ __forceinline__ void set(uint32_t *w, int i, float lo, float hi)
+    {
+        w[2 * i] = __float_as_uint(lo);
+        w[2 * i + 1] = __float_as_uint(hi);
+    }
+    static __device__ __forceinline__ uint32_t one(float v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ uint32_t raw(const float *p) { return __float_as_uint(*p); }
+};
+template <> struct Bits<__nv_bfloat16> {
+    static __device__ __forceinline__ float get(const uint32_t *w, int i)
+    {
+        return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    }
+    static __device__ __forceinline__ void set(uint32_t *w, int i, float lo, float hi)
+    {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        w[i] = *reinterpret_cast<const uint32_t *>(&v);
+    }
+    static __device__ __forceinline__ uint32_t one(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+    static __device__ __forceinline__ uint32_t raw(const __nv_bfloat16 *p) { return *reinterpret_cast<const unsigned short *>(p); }
+};
+template <> struct Bits<__half> {
+    static __device__ __forceinline__ float get(const uint32_t *w, int i)
+    {
+        return __half2float(__ushort_as_half(static_cast<unsigned short>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu)));
+    }
+    static __device__ __forceinline__ void set(uint32_t *w, int i, float lo, float hi)
+    {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        w[i] = *reinterpret_cast<const uint32_t *>(&v);
+    }
+    static __device__ __forceinline__ uint32_t one(float v) { return __half_as_ushort(__float2half_rn(v)); }
+    static __device__ __forceinline__ uint32_t raw(const __half *p) { return *reinterpret_cast<const unsigned short *>(p); }
+};
+template <typename T, int V>
+__device__ __forceinline__ float Pack<T, V>::get(int i) const { return Bits<T>::get(w, i); }
 
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack(const float (&f)[V])
+{
+    Pack<T, V> p;
+    if constexpr (V == 1) {
+        p.w[0] = Bits<T>::one(f[0]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) Bits<T>::set(p.w, i, f[2 * i], f[2 * i + 1]);
+    }
+    return p;
+}
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&f)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = p.get(i);
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> zero_pack()
+{
+    Pack<T, V> p;
+#pragma unroll
+    for (int i = 0; i < Pack<T, V>::W; ++i) p.w[i] = 0;
+    return p;
+}
 template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> load_pack(const T *p)
 {
-    return *reinterpret_cast<const Pack<T, V> *>(p);
+    Pack<T, V> r;
+    if constexpr (V * sizeof(T) == 2) {
+        r.w[0] = *reinterpret_cast<const unsigned short *>(p);
+    } else if constexpr (V * sizeof(T) == 4) {
+        r.w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else if constexpr (V * sizeof(T) == 8) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        r.w[0] = v.x;
+        r.w[1] = v.y;
+    } else {
+        static_assert(V * sizeof(T) == 16, "one access");
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        r.w[0] = v.x;
+        r.w[1] = v.y;
+        r.w[2] = v.z;
+        r.w[3] = v.w;
+    }
+    return r;
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &v)
 {
-    *reinterpret_cast<Pack<T, V> *>(p) = v;
+    if constexpr (V * sizeof(T) == 2) *reinterpret_cast<unsigned short *>(p) = static_cast<unsigned short>(v.w[0]);
+    else if constexpr (V * sizeof(T) == 4) *reinterpret_cast<uint32_t *>(p) = v.w[0];
+    else if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(v.w[0], v.w[1]);
+    else *reinterpret_cast<uint4 *>(p) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+}
+// V neighbouring elements of which the first `valid` may be read (the rest: zero); wide: they may move as one access
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_some(const T *p, int valid, bool wide)
+{
+    Pack<T, V> r = zero_pack<T, V>();
+    if (wide && valid >= V) {
+        r = load_pack<T, V>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < valid) r.w[i * sizeof(T) / 4] |= Bits<T>::raw(p + i) << (i * sizeof(T) % 4 * 8);
+    }
+    return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_some(T *p, const float (&f)[V], int valid, bool wide)
+{
+    if (wide && valid >= V) {
+        store_pack<T, V>(p, pack<T, V>(f));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < valid) p[i] = from_f32<T>(f[i]);
+    }
 }
 
 // ---- where sequences lie ------------------------------------------------------------------------------------
@@ -134,7 +247,7 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
 }
 
 // ---- elementary functions -------------------------------------------------------------------------------------
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.92596299e-8f;   // log2(e) as two floats
 
 __device__ __forceinline__ float exp2_fast(float x)          // 2^x, relative error about 2^-22
 {
@@ -152,7 +265,11 @@ __device__ __forceinline__ float rcp_fast(float x)           // 1/x, relative er
 // the odd series up to s^13 leaves 2e-8 of it and, unlike log2(1 + e), stays relatively exact for small e.
 __device__ __forceinline__ float softplus(float v)
 {
-    const float e = exp2_fast(-kLog2e * fabsf(v));
+    // exp(-|v|): what the rounded product with log2(e) loses comes back as a factor 1 + r ln 2
+    const float a = -fabsf(v), p0 = a * kLog2e;
+    const float rest = fmaf(a, kLog2eLow, fmaf(a, kLog2e, -p0));
+    float e = exp2_fast(p0);
+    e = fmaf(e, rest * 0.69314718f, e);
     const float s = e * rcp_fast(2.0f + e);
     const float q = s * s;
     float p = fmaf(q, 2.0f / 13.0f, 2.0f / 11.0f);

@@ -88,37 +88,6 @@ struct RawTok {
     Pack<T, VT> v[PP / VT];
 };
 
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> zero_pack()
-{
-    Pack<T, V> p;
-#pragma unroll
-    for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(0.0f);
-    return p;
-}
-// V neighbouring elements of which the first `valid` may be read
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> load_some(const T *p, int valid, bool wide)
-{
-    if (wide && valid >= V) return load_pack<T, V>(p);
-    Pack<T, V> r = zero_pack<T, V>();
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i < valid) r.v[i] = p[i];
-    return r;
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_some(T *p, const Pack<T, V> &v, int valid, bool wide)
-{
-    if (wide && valid >= V) {
-        store_pack<T, V>(p, v);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i < valid) p[i] = v.v[i];
-}
-
 // kMain: outputs.  kChunk: only a chunk's last state from zero and its sum of d.  kChunkBack: the same for the backward
 // recurrence, carry[t] = a[t] (carry[t+1] + dy'[t] C[t]), tokens walked from the last to the first; the launch passes dy as
 // u and C as B, and z (if any) turns dy into dy' = dy silu(z).
@@ -230,16 +199,16 @@ __global__ void __launch_bounds__(kScanThreads) scan_kernel(ScanArgs a)
                 const bool live = t0 + tt < t_end;
 #pragma unroll
                 for (int j = 0; j < VT; ++j) {
-                    const float uv = to_f32(ru.v[i].v[j]);
-                    float dv = to_f32(rd.v[i].v[j]) + dbias[j];
+                    const float uv = ru.v[i].get(j);
+                    float dv = rd.v[i].get(j) + dbias[j];
                     if (a.softplus) dv = softplus(dv);
                     if (!live) dv = 0.0f;                                // past the end: h stays as it is
-                    const float in = BACK ? (gate ? uv * silu(to_f32(rz.v[i].v[j])) : uv) : dv * uv;
+                    const float in = BACK ? (gate ? uv * silu(rz.v[i].get(j)) : uv) : dv * uv;
                     s_d[tt][pc + j] = make_float2(dv, in);
                     if (!MAIN) dtotal[j] += dv;
                     if (MAIN) {
                         skip[i * VT + j] = dskip[j] * uv;
-                        act[i * VT + j] = gate ? silu(to_f32(rz.v[i].v[j])) : 1.0f;
+                        act[i * VT + j] = gate ? silu(rz.v[i].get(j)) : 1.0f;
                     }
                 }
             }
@@ -251,8 +220,8 @@ __global__ void __launch_bounds__(kScanThreads) scan_kernel(ScanArgs a)
                 float *b = &s_b[e / NP][e % NP], *cc = &s_c[MAIN ? e / NP : 0][e % NP];
 #pragma unroll
                 for (int j = 0; j < VB; ++j) {
-                    b[j] = to_f32(rb.v[i].v[j]);
-                    if (MAIN) cc[j] = to_f32(rc.v[i].v[j]);
+                    b[j] = rb.v[i].get(j);
+                    if (MAIN) cc[j] = rc.v[i].get(j);
                 }
             }
         }
@@ -305,10 +274,9 @@ __global__ void __launch_bounds__(kScanThreads) scan_kernel(ScanArgs a)
                 const int e = (i * kScanThreads + tid) * VT;
                 const int tt = e / CB;
                 if (e < TT * CB && t0 + tt < t_end) {
-                    Pack<T, VT> out;
+                    float out[VT];
 #pragma unroll
-                    for (int j = 0; j < VT; ++j)
-                        out.v[j] = from_f32<T>((s_y[tt][pc + j] + skip[i * VT + j]) * act[i * VT + j]);
+                    for (int j = 0; j < VT; ++j) out[j] = (s_y[tt][pc + j] + skip[i * VT + j]) * act[i * VT + j];
                     store_some<T, VT>(y0 + (t0 + tt) * a.y.tstride, out, pvalid, a.wide_tok);
                 }
             }

@@ -167,12 +167,12 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
 #pragma unroll
                 for (int j = 0; j < VT; ++j) {
                     const int q = i * VT + j;
-                    const float raw = to_f32(rd.v[i].v[j]) + dbias[j], dout = to_f32(rg.v[i].v[j]);
-                    uv[q] = to_f32(ru.v[i].v[j]);
+                    const float raw = rd.v[i].get(j) + dbias[j], dout = rg.v[i].get(j);
+                    uv[q] = ru.v[i].get(j);
                     dv[q] = live ? (a.softplus ? softplus(raw) : raw) : 0.0f;
                     slope[q] = a.softplus ? sigmoid(raw) : 1.0f;
                     if (gate) {
-                        const float z = to_f32(rz.v[i].v[j]), sig = sigmoid(z);
+                        const float z = rz.v[i].get(j), sig = sigmoid(z);
                         dyv[q] = dout * z * sig;
                         zf[q] = dout * silu_slope(z, sig);
                     } else {
@@ -188,8 +188,8 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
             if (e < TB * NP) {
 #pragma unroll
                 for (int j = 0; j < VB; ++j) {
-                    s_b[e + j] = to_f32(rb.v[i].v[j]);
-                    s_c[e + j] = to_f32(rc.v[i].v[j]);
+                    s_b[e + j] = rb.v[i].get(j);
+                    s_c[e + j] = rc.v[i].get(j);
                 }
             }
         }
@@ -298,15 +298,15 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
             const int e = (i * NT + tid) * VT;
             const int tt = e / CB;
             if (e < TB * CB && t0 + tt < t_end) {
-                Pack<T, VT> odu, odd, odz;
+                float odu[VT], odd[VT], odz[VT];
 #pragma unroll
                 for (int j = 0; j < VT; ++j) {
                     const int q = i * VT + j, at = tt * YP + pc + j;
                     const float r1 = s_r1[at], r2 = s_r2[at] * 0.69314718055994531f;      // A2 is A log2(e)
                     const float dd = fmaf(uv[q], r1, r2) * slope[q];
-                    odu.v[j] = from_f32<T>(fmaf(dv[q], r1, dyv[q] * dskip[j]));
-                    odd.v[j] = from_f32<T>(dd);
-                    if (gate) odz.v[j] = from_f32<T>(fmaf(dskip[j], uv[q], s_y[at]) * zf[q]);
+                    odu[j] = fmaf(dv[q], r1, dyv[q] * dskip[j]);
+                    odd[j] = dd;
+                    if (gate) odz[j] = fmaf(dskip[j], uv[q], s_y[at]) * zf[q];
                     sum_b[j] += dd;
                     sum_d[j] = fmaf(dyv[q], uv[q], sum_d[j]);
                 }

@@ -74,8 +74,11 @@ long long scan_backward_workspace(const sysscan_args &a)
 }
 
 // ---- single tokens -------------------------------------------------------------------------------------------------
-// A channel's states are spread over LN lanes, four in each (one 128-bit access).  Bound: the state's traffic, 8 bytes per
-// (row, channel, state).
+// A warp takes 32 channels of one row.  Each lane first does what a channel costs once (softplus, gate) for one of them; then
+// the states pass in LN turns of 32/LN channels, LN lanes to a channel and four states to a lane (one 128-bit access: a turn
+// moves 512 contiguous bytes).  The lanes that share a channel in some turn own the LN channels of one residue, so a
+// turn's d and d u come from a neighbour by one shuffle, and the sums over the states go back the same way, transposed over
+// U turns at once.  Bound: the state's traffic, 8 bytes per (row, channel, state).
 namespace {
 
 constexpr int kStepThreads = 128;
@@ -95,46 +98,78 @@ template <typename T, int LN>
 __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(StepArgs a)
 {
     dependent_launch_enter();
+    constexpr int U = LN < 4 ? LN : 4, CW = 32 / LN;                      // turns in flight, channels per turn
     const long long row = blockIdx.y;
-    const int c = blockIdx.x * (kStepThreads / LN) + threadIdx.x / LN, ln = threadIdx.x % LN;
+    const int lane = threadIdx.x & 31, ln = lane % LN;
+    const int c0 = (blockIdx.x * (kStepThreads / 32) + (threadIdx.x >> 5)) * 32;
+    if (c0 >= a.channels) return;
+    const int c = c0 + ln * CW + lane / LN;                              // own channel: that of turn ln
     const bool own = c < a.channels;
     const long long slot = a.slot ? a.slot[row] : row;
-    const bool live = slot >= 0 && slot < a.slots;
     T *dst = static_cast<T *>(a.y) + row * a.y_stride + c;
-    if (!live) {
-        if (own && ln == 0) *dst = from_f32<T>(0.0f);
-        return;                                                          // the whole block: one row
+    if (slot < 0 || slot >= a.slots) {
+        if (own) *dst = from_f32<T>(0.0f);
+        return;
     }
-    float y = 0.0f;
-    float u = 0.0f;
+    float d = 0.0f, u = 0.0f, z = 0.0f, skip = 0.0f;
     if (own) {
-        const int n0 = ln * 4, g = c / a.per_group;
-        float *st = a.state + slot * a.state_stride + static_cast<long long>(c) * a.states + n0;
-        const float *A = a.A + static_cast<long long>(c) * a.states + n0;
-        const T *B = static_cast<const T *>(a.B) + row * a.b_stride + g * a.states + n0;
-        const T *C = static_cast<const T *>(a.C) + row * a.c_stride + g * a.states + n0;
-        const int valid = a.states - n0;
-        const Pack<float, 4> h0 = load_some<float, 4>(st, valid, a.wide), av = load_some<float, 4>(A, valid, a.wide);
-        const Pack<T, 4> bv = load_some<T, 4>(B, valid, a.wide), cv = load_some<T, 4>(C, valid, a.wide);
+        d = to_f32(static_cast<const T *>(a.delta)[row * a.delta_stride + c]);
         u = to_f32(static_cast<const T *>(a.u)[row * a.u_stride + c]);
-        float d = to_f32(static_cast<const T *>(a.delta)[row * a.delta_stride + c]) + (a.dbias ? a.dbias[c] : 0.0f);
-        if (a.softplus) d = softplus(d);
-        const float du = d * u;
-        Pack<float, 4> h;
+        if (a.z) z = to_f32(static_cast<const T *>(a.z)[row * a.z_stride + c]);
+        if (a.dbias) d += a.dbias[c];
+        if (a.D) skip = a.D[c];
+    }
+    const int n0 = ln * 4, valid_n = a.states - n0;
+    float *st = a.state + slot * a.state_stride + n0;
+    const T *B = static_cast<const T *>(a.B) + row * a.b_stride + n0, *C = static_cast<const T *>(a.C) + row * a.c_stride + n0;
+    const float *A = a.A + n0;
+    // with one group B and C are the same in every turn
+    const bool one_group = a.per_group == a.channels;
+    float bv[4], cv[4];
+    auto load_bc = [&](int g) {
+        const Pack<T, 4> b = load_some<T, 4>(B + g * a.states, valid_n, a.wide), cc = load_some<T, 4>(C + g * a.states, valid_n, a.wide);
+        unpack(b, bv);
+        unpack(cc, cv);
+    };
+    if (one_group) load_bc(0);
+    float y = 0.0f, du = 0.0f;
+#pragma unroll 1
+    for (int t0 = 0; t0 < LN; t0 += U) {
+        Pack<float, 4> h[U], av[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h.v[i] = fmaf(exp2_fast(d * (av.v[i] * kLog2e)), h0.v[i], du * to_f32(bv.v[i]));
-            y = i < valid ? fmaf(h.v[i], to_f32(cv.v[i]), y) : y;
+        for (int k = 0; k < U; ++k) {
+            const int ct = c0 + (t0 + k) * CW + lane / LN;
+            const int valid = ct < a.channels ? valid_n : 0;
+            h[k] = load_some<float, 4>(st + static_cast<long long>(ct) * a.states, valid, a.wide);
+            av[k] = load_some<float, 4>(A + static_cast<long long>(ct) * a.states, valid, a.wide);
         }
-        store_some<float, 4>(st, h, valid, a.wide);
-    }
+        if (t0 == 0) {                                                   // while the first states are on their way
+            if (a.softplus) d = softplus(d);
+            du = d * u;
+        }
+        float sums[U];
 #pragma unroll
-    for (int w = 1; w < LN; w *= 2) y += __shfl_xor_sync(kFullMask, y, w);
-    if (own && ln == 0) {
-        if (a.D) y = fmaf(a.D[c], u, y);
-        if (a.z) y *= silu(to_f32(static_cast<const T *>(a.z)[row * a.z_stride + c]));
-        *dst = from_f32<T>(y);
+        for (int k = 0; k < U; ++k) {
+            const int ct = c0 + (t0 + k) * CW + lane / LN;
+            const int from = lane - ln + t0 + k;
+            const float dt = __shfl_sync(kFullMask, d, from), dut = __shfl_sync(kFullMask, du, from);
+            if (!one_group && ct < a.channels) load_bc(ct / a.per_group);
+            float acc = 0.0f, hn[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hn[i] = fmaf(exp2_fast(dt * (av[k].get(i) * kLog2e)), h[k].get(i), dut * bv[i]);
+                if (i < valid_n) acc = fmaf(hn[i], cv[i], acc);
+            }
+            store_some<float, 4>(st + static_cast<long long>(ct) * a.states, hn, ct < a.channels ? valid_n : 0, a.wide);
+            sums[k] = acc;
+        }
+        const float v = sum_transposed<U, LN>(sums, lane);               // of turn t0 + lane % U
+        if (ln / U == t0 / U) y = v;
     }
+    if (!own) return;
+    y = fmaf(skip, u, y);
+    if (a.z) y *= silu(z);
+    *dst = from_f32<T>(y);
 }
 
 template <typename T, int LN>
@@ -155,7 +190,7 @@ cudaError_t launch_step(const StepArgs &k, long long rows, cudaStream_t s)
             q.state = k.state + r0 * k.state_stride;
             q.slots = k.slots - r0;
         }
-        const cudaError_t err = launch_kernel(scan_step_kernel<T, LN>, dim3(ceil_div(k.channels, kStepThreads / LN), static_cast<unsigned>(n)),
+        const cudaError_t err = launch_kernel(scan_step_kernel<T, LN>, dim3(ceil_div(k.channels, kStepThreads), static_cast<unsigned>(n)),
                                               dim3(kStepThreads), s, q);
         if (err != cudaSuccess) return err;
     }
