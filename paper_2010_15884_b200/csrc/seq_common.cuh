@@ -138,6 +138,18 @@ __device__ __forceinline__ Pack<T, V> load_some(const T *p, int valid, bool wide
     }
     return r;
 }
+// WIDE: the whole access or nothing
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ Pack<T, V> load_part(const T *p, int valid)
+{
+    if constexpr (WIDE) {
+        Pack<T, V> r = zero_pack<T, V>();
+        if (valid > 0) r = load_pack<T, V>(p);
+        return r;
+    } else {
+        return load_some<T, V>(p, valid, false);
+    }
+}
 template <typename T, int V>
 __device__ __forceinline__ void store_some(T *p, const float (&f)[V], int valid, bool wide)
 {
@@ -239,6 +251,12 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
 {
     f32x2 r;
@@ -280,6 +298,34 @@ __device__ __forceinline__ float softplus(float v)
     p = fmaf(q, p, 2.0f);
     return fmaf(s, p, fmaxf(v, 0.0f));
 }
+// the same for two values, packed wherever the machine can
+__device__ __forceinline__ f32x2 softplus2(f32x2 v)
+{
+    const float2 f = halves(v);
+    const f32x2 a = pair(-fabsf(f.x), -fabsf(f.y)), l = pair(kLog2e, kLog2e);
+    const f32x2 p0 = mul2(a, l);
+    const float2 p = halves(p0);
+    const f32x2 rest = fma2(a, pair(kLog2eLow, kLog2eLow), fma2(a, l, pair(-p.x, -p.y)));
+    f32x2 e = pair(exp2_fast(p.x), exp2_fast(p.y));
+    e = fma2(e, mul2(rest, pair(0.69314718f, 0.69314718f)), e);
+    const float2 w = halves(add2(e, pair(2.0f, 2.0f)));
+    const f32x2 s = mul2(e, pair(rcp_fast(w.x), rcp_fast(w.y)));
+    const f32x2 q = mul2(s, s);
+    f32x2 r = fma2(q, pair(2.0f / 13.0f, 2.0f / 13.0f), pair(2.0f / 11.0f, 2.0f / 11.0f));
+    r = fma2(q, r, pair(2.0f / 9.0f, 2.0f / 9.0f));
+    r = fma2(q, r, pair(2.0f / 7.0f, 2.0f / 7.0f));
+    r = fma2(q, r, pair(2.0f / 5.0f, 2.0f / 5.0f));
+    r = fma2(q, r, pair(2.0f / 3.0f, 2.0f / 3.0f));
+    r = fma2(q, r, pair(2.0f, 2.0f));
+    return fma2(s, r, pair(fmaxf(f.x, 0.0f), fmaxf(f.y, 0.0f)));
+}
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 v)
+{
+    const float2 p = halves(mul2(v, pair(-kLog2e, -kLog2e)));
+    const float2 w = halves(add2(pair(exp2_fast(p.x), exp2_fast(p.y)), pair(1.0f, 1.0f)));
+    return pair(rcp_fast(w.x), rcp_fast(w.y));
+}
+__device__ __forceinline__ f32x2 silu2(f32x2 v) { return mul2(v, sigmoid2(v)); }
 __device__ __forceinline__ float sigmoid(float v) { return rcp_fast(1.0f + exp2_fast(-kLog2e * v)); }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
 __device__ __forceinline__ float silu_slope(float v, float sig) { return sig * fmaf(v, 1.0f - sig, 1.0f); }
@@ -289,6 +335,27 @@ void count_launches(int n);                  // sysconv_api.cu
 int device_sm_count();                       // 0: no device
 
 inline int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+
+// launch_kernel with dynamic shared memory
+template <typename... KArgs, typename... Args>
+cudaError_t launch_kernel_smem(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t bytes, cudaStream_t s, Args &&...args)
+{
+    if (bytes > 48 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+        if (err != cudaSuccess) return err;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent_launch_enabled() ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
 
 // Calls f with a null pointer of the token type `type`.
 template <typename F>

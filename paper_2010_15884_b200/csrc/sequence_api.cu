@@ -51,6 +51,7 @@ int check_scan(const sysscan_args *a, bool backward)
     if (st != SYSCONV_OK) return st;
     if (a->channels < 1 || a->states < 1 || a->groups < 1 || a->channels % a->groups != 0 || !valid_type(a->type) || !a->A)
         return SYSCONV_EINVAL;
+    if (a->seq.length > (1LL << 30) || a->seq.total > (1LL << 30)) return SYSCONV_EUNSUPPORTED;
     if (a->states > kMaxStates || a->seq.sequences > 65535 || a->channels > (1LL << 30) / a->states) return SYSCONV_EUNSUPPORTED;
     const long long bc = a->groups * a->states;
     if (!valid_tokens(a->u, a->seq, a->channels, false) || !valid_tokens(a->delta, a->seq, a->channels, false) ||

@@ -1,11 +1,12 @@
 // Selective state space scan, forward: h[t][n] = exp(d[t] A[n]) h[t-1][n] + d[t] u[t] B[t][n], y[t] = C[t].h[t] + D u[t].
 //
-// Mapping.  A channel's states are spread over LN neighbouring lanes, S of them in each lane's registers (pairs, so that
-// one packed instruction updates two); a block is 128 threads = 128/LN channels of one sequence and marches along the
-// tokens.  A tile of TT tokens is staged in shared memory: while it is staged every (token, channel) has softplus and
-// the gate computed once; B and C are widened to fp32.  The recurrence then reads one (d, d u) pair per channel and S
-// values of B and C per lane and token.  The sums over n of U tokens are transposed and added over the LN lanes together
-// (U-1 shuffles for U tokens).  The next tile's loads are in flight while the current tile is computed.
+// Mapping.  A block takes 128/LN channels of one sequence and marches along the tokens in tiles of TT.  Its eight warps have
+// two jobs.  Four run the recurrence: a channel's states are spread over LN neighbouring lanes, S of them in each lane's
+// registers (pairs, so that one packed instruction updates two); per token a lane reads its channel's (d, d u) and S values
+// of B and C from shared memory, and the sums over n of U tokens are transposed and added over the LN lanes together
+// (U-1 shuffles for U tokens).  The other four fetch, compute softplus and gate once per (token, channel), widen B and C,
+// and finish and store the outputs, one tile ahead of and one behind the recurrence (two buffers; four named barriers).
+// The recurrence alone is a chain that one warp per scheduler cannot hide; the second job's instructions fill its gaps.
 //
 // Bound: the exponentials.  A (token, channel, state) costs one exp and four fp32 operations; the special function unit
 // gives 16 results per clock and SM, so T x channels x states / (148 x 16 x 1.965 GHz) is the floor.
@@ -19,7 +20,11 @@
 
 namespace sysconv {
 
-constexpr int kScanThreads = 128;
+constexpr int kScanThreads = 128;                // threads of each job
+
+// Named barriers of a block: `wait` joins, `arrive` only counts; the writes before either are visible after `wait`.
+__device__ __forceinline__ void bar_wait(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(2 * kScanThreads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(2 * kScanThreads) : "memory"); }
 
 struct ScanArgs {
     SeqMap map;
@@ -73,13 +78,25 @@ struct ScanShape {
     static constexpr int NP = LN * S;                                   // states, padded
     static constexpr int CB = kScanThreads / LN;                        // channels per block
     static constexpr int U = LN < 16 ? LN : 16;                         // tokens whose sums are added together
-    static constexpr int TT0 = NP <= 2 ? 8 : (NP <= 4 ? 16 : 32);
-    static constexpr int TT = NP >= 128 ? 16 : TT0;                     // tokens per tile
+    static constexpr int TT = LN < 4 || NP >= 64 ? 16 : 32;             // tokens per tile
     static constexpr int PP = (TT * CB + kScanThreads - 1) / kScanThreads;   // (token, channel) pairs per thread
     static constexpr int VT = PP >= 4 ? 4 : (PP >= 2 ? 2 : 1);          // ... of them neighbouring channels
     static constexpr int BE = (TT * NP + kScanThreads - 1) / kScanThreads;   // elements of B per thread
     static constexpr int VB = BE >= 4 ? 4 : (BE >= 2 ? 2 : 1);
-    static constexpr int YP = CB + 32 / LN;                             // pitch of the sums: conflict-free for the lanes' writes
+    // pitch of the sums: the lanes' writes fall in different banks, and VT of them can be read at once
+    static constexpr int YP = CB + (32 / LN > VT ? 32 / LN : VT);
+};
+
+// A tile in shared memory.  B and C stay in the tokens' type: a lane's read returns one 32-bit word per clock and SM
+// quarter whatever its width and however many lanes share the address, and with B and C as fp32 those reads, not the
+// exponentials, bound the recurrence (measured on 4096 channels x 16 states: 8.8 words per token and warp against 16
+// clocks of exponentials).
+template <typename T, int LN, int S, bool MAIN>
+struct alignas(16) ScanTile {
+    using G = ScanShape<LN, S>;
+    float2 d[G::TT][G::CB];                                              // d, d u
+    T b[G::TT][G::NP], c[MAIN ? G::TT : 1][G::NP];
+    float y[MAIN ? G::TT : 1][G::YP];
 };
 
 // A tile's raw values in registers
@@ -92,21 +109,25 @@ struct RawTok {
 // recurrence, carry[t] = a[t] (carry[t+1] + dy'[t] C[t]), tokens walked from the last to the first; the launch passes dy as
 // u and C as B, and z (if any) turns dy into dy' = dy silu(z).
 enum ScanMode { kMain, kChunk, kChunkBack };
-template <typename T, int LN, int S, int MODE>
-__global__ void __launch_bounds__(kScanThreads) scan_kernel(ScanArgs a)
+// WIDE: rows and channel counts allow whole accesses everywhere.
+template <typename T, int LN, int S, int MODE, bool WIDE>
+__global__ void __launch_bounds__(2 * kScanThreads, 2) scan_kernel(ScanArgs a)
 {
     using G = ScanShape<LN, S>;
     constexpr bool MAIN = MODE == kMain, BACK = MODE == kChunkBack;
-    constexpr int NP = G::NP, CB = G::CB, U = G::U, TT = G::TT, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB, YP = G::YP;
+    constexpr int NP = G::NP, CB = G::CB, U = G::U, TT = G::TT, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB;
     constexpr int P2 = S / 2;
-    static_assert(TT % U == 0 && PP % VT == 0 && BE % VB == 0, "tile shape");
-    __shared__ float2 s_d[TT][CB];                                       // d, d u
-    __shared__ __align__(16) float s_b[TT][NP];
-    __shared__ __align__(16) float s_c[MAIN ? TT : 1][NP];
-    __shared__ float s_y[MAIN ? TT : 1][YP];
+    static_assert(sizeof(ScanTile<T, LN, S, MAIN>) % 16 == 0 && (G::TT * G::CB * 8) % 16 == 0 && (G::TT * G::NP * sizeof(T)) % 16 == 0, "alignment");
+    static_assert((kScanThreads * VT % CB == 0 || PP == VT) && (kScanThreads * VB % NP == 0 || BE == VB), "a thread's accesses share a column");
+    static_assert(TT % U == 0 && TT % kScanBlock == 0 && PP % VT == 0 && BE % VB == 0, "tile shape");
+    using Tile = ScanTile<T, LN, S, MAIN>;
+    extern __shared__ __align__(16) float scan_smem[];
+    Tile *tiles = reinterpret_cast<Tile *>(scan_smem);                   // two
+    enum { kFull = 1, kDone = 3 };                                       // barriers: + buffer
     dependent_launch_enter();
 
-    const int tid = threadIdx.x, lane = tid & 31;
+    const bool producer = threadIdx.x >= kScanThreads;
+    const int tid = threadIdx.x & (kScanThreads - 1), lane = tid & 31;
     const int g = blockIdx.x / a.blocks_per_group;
     const int c0 = g * a.per_group + (blockIdx.x - g * a.blocks_per_group) * CB;      // first channel of the block
     const int c_end = min((g + 1) * a.per_group, a.channels);
@@ -119,203 +140,255 @@ __global__ void __launch_bounds__(kScanThreads) scan_kernel(ScanArgs a)
     if (t_begin >= length && blockIdx.z > 0) return;
     if (MODE == kChunk && last_chunk) return;                            // nothing follows it
     if (BACK && blockIdx.z == 0) return;
-
-    const int cl = tid / LN, ln = tid % LN;                              // own channel and states in the recurrence
-    const int c = c0 + cl;
-    const bool own = c < c_end;
-    f32x2 A2[P2], h[P2];
     const long long chain = static_cast<long long>(r) * a.chunks + blockIdx.z;
-    {
-        float av[S], hv[S];
-        const float *from = nullptr;                                     // [channels][states]
-        if (MAIN && a.chunks > 1) from = a.carry + chain * a.channels * a.states;
-        else if (MAIN && a.state) from = a.state + static_cast<long long>(r) * a.channels * a.states;
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const int n = ln * S + i;
-            const long long at = static_cast<long long>(c) * a.states + n;
-            const bool ok = own && n < a.states;
-            av[i] = ok ? decay_rate(a.A[at]) : 0.0f;
-            hv[i] = ok && from ? from[at] : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < P2; ++i) {
-            A2[i] = pair(av[2 * i], av[2 * i + 1]);
-            h[i] = pair(hv[2 * i], hv[2 * i + 1]);
-        }
-    }
+    const int tile_count = static_cast<int>((t_end - t_begin + TT - 1) / TT);
 
-    // the pairs this thread stages and finishes: VT neighbouring channels, the same ones in every tile
-    const int pc = (tid * VT) % CB;                                      // (only if PP * 128 covers the tile exactly)
-    const T *B0 = token_row<T>(a.B, a.map, r, first) + g * a.states;
-    const T *C0 = MAIN ? token_row<T>(a.C, a.map, r, first) + g * a.states : nullptr;
-    const T *u0 = token_row<T>(a.u, a.map, r, first) + c0 + pc;
-    const T *d0 = token_row<T>(a.delta, a.map, r, first) + c0 + pc;
-    const bool gate = MODE != kChunk && a.z.ptr != nullptr;
-    const T *z0 = gate ? token_row<T>(a.z, a.map, r, first) + c0 + pc : nullptr;
-    T *y0 = MAIN ? token_row<T>(a.y, a.map, r, first) + c0 + pc : nullptr;
-    const int pvalid = c_end - c0 - pc;                                  // channels of the pairs that exist
-    float dbias[VT], dskip[VT], dtotal[VT];
+    if (producer) {
+        // the pairs this thread stages and finishes: VT neighbouring channels, the same ones in every tile
+        const int pc = (tid * VT) % CB;
+        const int pvalid = c_end - c0 - pc;                              // channels of the pairs that exist
+        const bool gate = MODE != kChunk && a.z.ptr != nullptr;
+        const bool pairs = tid * VT < TT * CB;                           // (the smallest tiles have fewer pairs than threads)
+        const bool cells = tid * VB < TT * NP;
+        // addresses of this thread's first pair and first B, C element; tokens run backwards in the backward recurrence
+        constexpr int dir = BACK ? -1 : 1;
+        const int p_row = tid * VT / CB, bc_row = tid * VB / NP, bc_n = tid * VB % NP;
+        constexpr int p_step = kScanThreads * VT / CB, bc_step = kScanThreads * VB / NP;   // rows between a thread's accesses
+        const long long t_first = BACK ? t_end - 1 : t_begin;
+        auto at = [&](const Tokens &x, int row, int col) {
+            return token_row<T>(x, a.map, r, first) + (t_first + dir * row) * x.tstride + col;
+        };
+        const T *pu = at(a.u, p_row, c0 + pc), *pd = at(a.delta, p_row, c0 + pc), *pz = gate ? at(a.z, p_row, c0 + pc) : nullptr;
+        const T *pb = at(a.B, bc_row, g * a.states + bc_n), *pcc = MAIN ? at(a.C, bc_row, g * a.states + bc_n) : nullptr;
+        T *py = MAIN ? at(a.y, p_row, c0 + pc) : nullptr;
+        float dbias[VT], dskip[VT], dtotal[VT];
 #pragma unroll
-    for (int j = 0; j < VT; ++j) {
-        const bool ok = j < pvalid;
-        dbias[j] = ok && a.dbias ? a.dbias[c0 + pc + j] : 0.0f;
-        dskip[j] = MAIN && ok && a.D ? a.D[c0 + pc + j] : 0.0f;
-        dtotal[j] = 0.0f;
-    }
-    float *saved = MAIN && a.saved ? a.saved + saved_base(a.map, r, first) * a.channels * a.states : nullptr;
-
-    RawTok<T, PP, VT> ru, rd, rz;
-    RawTok<T, BE, VB> rb, rc;
-    auto fetch = [&](long long t0) {
-#pragma unroll
-        for (int i = 0; i < PP / VT; ++i) {
-            const int e = (i * kScanThreads + tid) * VT;
-            const long long walk = t0 + e / CB, t = BACK ? t_begin + t_end - 1 - walk : walk;
-            const int valid = e < TT * CB && walk < t_end ? pvalid : 0;
-            ru.v[i] = load_some<T, VT>(u0 + t * a.u.tstride, valid, a.wide_tok);
-            rd.v[i] = load_some<T, VT>(d0 + t * a.delta.tstride, valid, a.wide_tok);
-            if (gate) rz.v[i] = load_some<T, VT>(z0 + t * a.z.tstride, valid, a.wide_tok);
+        for (int j = 0; j < VT; ++j) {
+            const bool ok = j < pvalid;
+            dbias[j] = ok && a.dbias ? a.dbias[c0 + pc + j] : 0.0f;
+            dskip[j] = MAIN && ok && a.D ? a.D[c0 + pc + j] : 0.0f;
+            dtotal[j] = 0.0f;
         }
-#pragma unroll
-        for (int i = 0; i < BE / VB; ++i) {
-            const int e = (i * kScanThreads + tid) * VB;
-            const long long walk = t0 + e / NP, t = BACK ? t_begin + t_end - 1 - walk : walk;
-            const int n = e % NP;
-            const int valid = e < TT * NP && walk < t_end ? a.states - n : 0;
-            rb.v[i] = load_some<T, VB>(B0 + t * a.B.tstride + n, valid, a.wide_bc);
-            if (MAIN) rc.v[i] = load_some<T, VB>(C0 + t * a.C.tstride + n, valid, a.wide_bc);
-        }
-    };
-    if (t_begin < t_end) fetch(t_begin);
-    for (long long t0 = t_begin; t0 < t_end; t0 += TT) {
-        // stage the tile; keep what the outputs need
-        float skip[PP], act[PP];
-#pragma unroll
-        for (int i = 0; i < PP / VT; ++i) {
-            const int e = (i * kScanThreads + tid) * VT;
-            if (e < TT * CB) {
-                const int tt = e / CB;
-                const bool live = t0 + tt < t_end;
-#pragma unroll
-                for (int j = 0; j < VT; ++j) {
-                    const float uv = ru.v[i].get(j);
-                    float dv = rd.v[i].get(j) + dbias[j];
-                    if (a.softplus) dv = softplus(dv);
-                    if (!live) dv = 0.0f;                                // past the end: h stays as it is
-                    const float in = BACK ? (gate ? uv * silu(rz.v[i].get(j)) : uv) : dv * uv;
-                    s_d[tt][pc + j] = make_float2(dv, in);
-                    if (!MAIN) dtotal[j] += dv;
-                    if (MAIN) {
-                        skip[i * VT + j] = dskip[j] * uv;
-                        act[i * VT + j] = gate ? silu(rz.v[i].get(j)) : 1.0f;
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < BE / VB; ++i) {
-            const int e = (i * kScanThreads + tid) * VB;
-            if (e < TT * NP) {
-                float *b = &s_b[e / NP][e % NP], *cc = &s_c[MAIN ? e / NP : 0][e % NP];
-#pragma unroll
-                for (int j = 0; j < VB; ++j) {
-                    b[j] = rb.v[i].get(j);
-                    if (MAIN) cc[j] = rc.v[i].get(j);
-                }
-            }
-        }
-        __syncthreads();
-        if (t0 + TT < t_end) fetch(t0 + TT);
-
-#pragma unroll 1
-        for (int tu = 0; tu < TT; tu += U) {
-            if (saved != nullptr && ((t0 + tu) & (kScanBlock - 1)) == 0 && t0 + tu < t_end && own) {
-                float *to = saved + ((t0 + tu) / kScanBlock * a.channels + c) * a.states;
-#pragma unroll
-                for (int i = 0; i < P2; ++i) {
-                    const float2 v = halves(h[i]);
-                    if (ln * S + 2 * i < a.states) to[ln * S + 2 * i] = v.x;
-                    if (ln * S + 2 * i + 1 < a.states) to[ln * S + 2 * i + 1] = v.y;
-                }
-            }
-            float sums[U];
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const float2 d = s_d[tu + k][cl];
-                const f32x2 dd = pair(d.x, d.x), du = pair(d.y, d.y);
-                f32x2 acc;
-#pragma unroll
-                for (int i = 0; i < P2; ++i) {
-                    const float2 b = *reinterpret_cast<const float2 *>(&s_b[tu + k][ln * S + 2 * i]);
-                    const float2 x = halves(mul2(A2[i], dd));
-                    const f32x2 decay = pair(exp2_fast(x.x), exp2_fast(x.y));
-                    if (BACK) h[i] = mul2(decay, fma2(pair(b.x, b.y), du, h[i]));
-                    else h[i] = fma2(decay, h[i], mul2(pair(b.x, b.y), du));
-                    if (MAIN) {
-                        const float2 cc = *reinterpret_cast<const float2 *>(&s_c[tu + k][ln * S + 2 * i]);
-                        acc = i == 0 ? mul2(h[i], pair(cc.x, cc.y)) : fma2(h[i], pair(cc.x, cc.y), acc);
-                    }
-                }
-                if (MAIN) {
-                    const float2 v = halves(acc);
-                    sums[k] = v.x + v.y;
-                }
-            }
-            if (MAIN) {
-                const float v = sum_transposed<U, LN>(sums, lane);
-                if (LN <= U || ln < U) s_y[tu + ln % U][cl] = v;
-            }
-        }
-        __syncthreads();
-        if (MAIN) {
+        RawTok<T, PP, VT> ru, rd, rz;
+        RawTok<T, BE, VB> rb, rc;
+        int left = static_cast<int>(t_end - t_begin);                    // tokens not fetched yet
+        auto fetch = [&]() {
 #pragma unroll
             for (int i = 0; i < PP / VT; ++i) {
-                const int e = (i * kScanThreads + tid) * VT;
-                const int tt = e / CB;
-                if (e < TT * CB && t0 + tt < t_end) {
-                    float out[VT];
+                const int valid = pairs && p_row + i * p_step < left ? pvalid : 0;
+                ru.v[i] = load_part<T, VT, WIDE>(pu + dir * i * p_step * a.u.tstride, valid);
+                rd.v[i] = load_part<T, VT, WIDE>(pd + dir * i * p_step * a.delta.tstride, valid);
+                if (gate) rz.v[i] = load_part<T, VT, WIDE>(pz + dir * i * p_step * a.z.tstride, valid);
+            }
 #pragma unroll
-                    for (int j = 0; j < VT; ++j) out[j] = (s_y[tt][pc + j] + skip[i * VT + j]) * act[i * VT + j];
-                    store_some<T, VT>(y0 + (t0 + tt) * a.y.tstride, out, pvalid, a.wide_tok);
+            for (int i = 0; i < BE / VB; ++i) {
+                const int valid = cells && bc_row + i * bc_step < left ? a.states - bc_n : 0;
+                rb.v[i] = load_part<T, VB, WIDE>(pb + dir * i * bc_step * a.B.tstride, valid);
+                if (MAIN) rc.v[i] = load_part<T, VB, WIDE>(pcc + dir * i * bc_step * a.C.tstride, valid);
+            }
+            pu += dir * TT * a.u.tstride;
+            pd += dir * TT * a.delta.tstride;
+            if (gate) pz += dir * TT * a.z.tstride;
+            pb += dir * TT * a.B.tstride;
+            if (MAIN) pcc += dir * TT * a.C.tstride;
+            left -= TT;
+        };
+        // what the outputs of a staged tile need: D u and silu(z)
+        float skip0[PP], act0[PP], skip1[PP], act1[PP];
+        auto stage = [&](Tile &s, int live, float (&skip)[PP], float (&act)[PP]) {       // live: tokens of the tile
+#pragma unroll
+            for (int i = 0; i < PP / VT; ++i) {
+                const int row = p_row + i * p_step;
+                float uv[VT], dv[VT], in[VT], zv[VT];
+                unpack(ru.v[i], uv);
+                unpack(rd.v[i], dv);
+                if (gate) unpack(rz.v[i], zv);
+                if constexpr (VT > 1) {
+#pragma unroll
+                    for (int j = 0; j < VT; j += 2) {
+                        f32x2 d = add2(pair(dv[j], dv[j + 1]), pair(dbias[j], dbias[j + 1]));
+                        if (a.softplus) d = softplus2(d);
+                        const float2 f = halves(d);
+                        dv[j] = f.x;
+                        dv[j + 1] = f.y;
+                        if (gate) {
+                            const float2 w = halves(silu2(pair(zv[j], zv[j + 1])));
+                            zv[j] = w.x;
+                            zv[j + 1] = w.y;
+                        }
+                    }
+                } else {
+                    dv[0] += dbias[0];
+                    if (a.softplus) dv[0] = softplus(dv[0]);
+                    if (gate) zv[0] = silu(zv[0]);
+                }
+#pragma unroll
+                for (int j = 0; j < VT; ++j) {
+                    if (row >= live) dv[j] = 0.0f;                       // past the end: h stays as it is
+                    in[j] = BACK ? (gate ? uv[j] * zv[j] : uv[j]) : dv[j] * uv[j];
+                    if (!MAIN && pairs) dtotal[j] += dv[j];
+                    if (MAIN) {
+                        skip[i * VT + j] = dskip[j] * uv[j];
+                        act[i * VT + j] = gate ? zv[j] : 1.0f;
+                    }
+                }
+                if (pairs) {
+                    if constexpr (VT > 1) {
+#pragma unroll
+                        for (int j = 0; j < VT; j += 2)
+                            *reinterpret_cast<float4 *>(&s.d[row][pc + j]) = make_float4(dv[j], in[j], dv[j + 1], in[j + 1]);
+                    } else {
+                        s.d[row][pc] = make_float2(dv[0], in[0]);
+                    }
                 }
             }
+            if (cells) {
+#pragma unroll
+                for (int i = 0; i < BE / VB; ++i) {
+                    store_pack<T, VB>(&s.b[bc_row + i * bc_step][bc_n], rb.v[i]);
+                    if (MAIN) store_pack<T, VB>(&s.c[bc_row + i * bc_step][bc_n], rc.v[i]);
+                }
+            }
+        };
+        auto finish = [&](Tile &s, int live, const float (&skip)[PP], const float (&act)[PP]) {
+            if (!MAIN) return;
+#pragma unroll
+            for (int i = 0; i < PP / VT; ++i) {
+                const int row = p_row + i * p_step;
+                if (pairs && row < live) {
+                    float out[VT];
+                    unpack(load_pack<float, VT>(&s.y[row][pc]), out);
+#pragma unroll
+                    for (int j = 0; j < VT; ++j) out[j] = (out[j] + skip[i * VT + j]) * act[i * VT + j];
+                    if constexpr (WIDE) {
+                        if (pvalid > 0) store_pack<T, VT>(py + i * p_step * a.y.tstride, pack<T, VT>(out));
+                    } else {
+                        store_some<T, VT>(py + i * p_step * a.y.tstride, out, pvalid, false);
+                    }
+                }
+            }
+            py += TT * a.y.tstride;
+        };
+        // stage tile k, then finish tile k - 1, whose successor the recurrence works on meanwhile.  Buffer k % 2 was left by
+        // tile k - 2, which was finished in the round before.
+        if (tile_count > 0) fetch();
+        int k = 0, live = static_cast<int>(t_end - t_begin);
+        auto round = [&](int buf, float (&skip)[PP], float (&act)[PP], const float (&skip_old)[PP], const float (&act_old)[PP]) {
+            if (k < tile_count) {
+                stage(tiles[buf], live, skip, act);
+                bar_arrive(kFull + buf);
+                if (k + 1 < tile_count) fetch();
+            }
+            if (k > 0) {
+                bar_wait(kDone + (buf ^ 1));
+                finish(tiles[buf ^ 1], live + TT, skip_old, act_old);
+            }
+            live -= TT;
+            ++k;
+        };
+        while (k <= tile_count) {
+            round(0, skip0, act0, skip1, act1);
+            if (k <= tile_count) round(1, skip1, act1, skip0, act0);
         }
-    }
-
-    if (MAIN) {
-        if (a.final_state != nullptr && last_chunk && own) {
-            float *to = a.final_state + (static_cast<long long>(r) * a.channels + c) * a.states;
+        if (!MAIN) {                                                     // the sums of d: every tile has been used by now
+            float *part = reinterpret_cast<float *>(tiles);              // [threads][VT]
+#pragma unroll
+            for (int j = 0; j < VT; ++j) part[tid * VT + j] = dtotal[j];
+        }
+    } else {
+        const int cl = tid / LN, ln = tid % LN, c = c0 + cl;             // own channel and states
+        const bool own = c < c_end;
+        f32x2 A2[P2], h[P2];
+        {
+            float av[S], hv[S];
+            const float *from = nullptr;                                 // [channels][states]
+            if (MAIN && a.chunks > 1) from = a.carry + chain * a.channels * a.states;
+            else if (MAIN && a.state) from = a.state + static_cast<long long>(r) * a.channels * a.states;
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                const int n = ln * S + i;
+                const long long at = static_cast<long long>(c) * a.states + n;
+                const bool ok = own && n < a.states;
+                av[i] = ok ? decay_rate(a.A[at]) : 0.0f;
+                hv[i] = ok && from ? from[at] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < P2; ++i) {
+                A2[i] = pair(av[2 * i], av[2 * i + 1]);
+                h[i] = pair(hv[2 * i], hv[2 * i + 1]);
+            }
+        }
+        auto put = [&](float *to) {
 #pragma unroll
             for (int i = 0; i < P2; ++i) {
                 const float2 v = halves(h[i]);
                 if (ln * S + 2 * i < a.states) to[ln * S + 2 * i] = v.x;
                 if (ln * S + 2 * i + 1 < a.states) to[ln * S + 2 * i + 1] = v.y;
             }
-        }
-        return;
-    }
-    // chunk: last state, and the sum of d over its tokens
-    if (own) {
-        float *to = a.carry + (chain * a.channels + c) * a.states;
+        };
+        float *saved = MAIN && a.saved && own ? a.saved + (saved_base(a.map, r, first) * a.channels + c) * a.states : nullptr;
+        for (int k = 0; k < tile_count; ++k) {
+            Tile &s = tiles[k & 1];
+            const long long t0 = t_begin + static_cast<long long>(k) * TT;
+            bar_wait(kFull + (k & 1));
+            // blocks of 16 tokens without a branch inside, so that one token's loads, another's exponentials and a third's
+            // sums overlap in one warp
+#pragma unroll 1
+            for (int tb = 0; tb < TT; tb += kScanBlock) {
+                if (saved != nullptr && t0 + tb < t_end) put(saved + (t0 + tb) / kScanBlock * a.channels * a.states);
+                float y[kScanBlock / U];                                 // stored last: no load waits behind a store
 #pragma unroll
-        for (int i = 0; i < P2; ++i) {
-            const float2 v = halves(h[i]);
-            if (ln * S + 2 * i < a.states) to[ln * S + 2 * i] = v.x;
-            if (ln * S + 2 * i + 1 < a.states) to[ln * S + 2 * i + 1] = v.y;
+                for (int tu = tb; tu < tb + kScanBlock; tu += U) {
+                    float sums[U];
+#pragma unroll
+                    for (int q = 0; q < U; ++q) {
+                        const float2 d = s.d[tu + q][cl];
+                        const f32x2 dd = pair(d.x, d.x), du = pair(d.y, d.y);
+                        const Pack<T, S> b = load_pack<T, S>(&s.b[tu + q][ln * S]);
+                        Pack<T, S> cc;
+                        if (MAIN) cc = load_pack<T, S>(&s.c[tu + q][ln * S]);
+                        f32x2 acc;
+#pragma unroll
+                        for (int i = 0; i < P2; ++i) {
+                            const f32x2 bv = pair(b.get(2 * i), b.get(2 * i + 1));
+                            const float2 x = halves(mul2(A2[i], dd));
+                            const f32x2 decay = pair(exp2_fast(x.x), exp2_fast(x.y));
+                            if (BACK) h[i] = mul2(decay, fma2(bv, du, h[i]));
+                            else h[i] = fma2(decay, h[i], mul2(bv, du));
+                            if (MAIN) {
+                                const f32x2 cv = pair(cc.get(2 * i), cc.get(2 * i + 1));
+                                acc = i == 0 ? mul2(h[i], cv) : fma2(h[i], cv, acc);
+                            }
+                        }
+                        if (MAIN) {
+                            const float2 v = halves(acc);
+                            sums[q] = v.x + v.y;
+                        }
+                    }
+                    if (MAIN) y[(tu - tb) / U] = sum_transposed<U, LN>(sums, lane);
+                }
+                if (MAIN && (LN <= U || ln < U)) {
+#pragma unroll
+                    for (int i = 0; i < kScanBlock / U; ++i) s.y[tb + i * U + ln % U][cl] = y[i];
+                }
+            }
+            bar_arrive(kDone + (k & 1));
+        }
+        if (MAIN) {
+            if (a.final_state != nullptr && last_chunk && own) put(a.final_state + (static_cast<long long>(r) * a.channels + c) * a.states);
+        } else if (own) {
+            put(a.carry + (chain * a.channels + c) * a.states);
         }
     }
+    if (MAIN) return;
     __syncthreads();
-    float *part = reinterpret_cast<float *>(s_d);                        // [threads][VT]
-#pragma unroll
-    for (int j = 0; j < VT; ++j) part[tid * VT + j] = dtotal[j];
-    __syncthreads();
-    if (tid < CB && c0 + tid < c_end) {
-        // threads whose pairs are this channel: tid' * VT = channel - j mod CB
+    if (threadIdx.x < CB && c0 + static_cast<int>(threadIdx.x) < c_end) {
+        // producers whose pairs are this channel
+        const float *part = reinterpret_cast<const float *>(tiles);
         float v = 0.0f;
-        const int j = tid % VT;
-        for (int w = tid / VT; w < kScanThreads; w += CB / VT) v += part[w * VT + j];
-        a.dsum[chain * a.channels + c0 + tid] = v;
+        const int j = threadIdx.x % VT;
+        for (int w = threadIdx.x / VT; w < kScanThreads; w += CB / VT) v += part[w * VT + j];
+        a.dsum[chain * a.channels + c0 + threadIdx.x] = v;
     }
 }
 
@@ -358,15 +431,15 @@ inline int padded_states(long long n)
 
 ScanPlan scan_plan(const sysscan_args &a);
 
-template <typename T, int LN, int S>
-cudaError_t launch_scan_shape(const ScanArgs &k, cudaStream_t s, int *launches)
+template <typename T, int LN, int S, bool WIDE>
+cudaError_t launch_scan_wide(const ScanArgs &k, cudaStream_t s, int *launches)
 {
     using G = ScanShape<LN, S>;
     ScanArgs a = k;
     a.blocks_per_group = ceil_div(a.per_group, G::CB);
     const dim3 grid(a.blocks_per_group * a.groups, a.map.sequences, a.chunks);
     if (a.chunks > 1) {
-        cudaError_t err = launch_kernel(scan_kernel<T, LN, S, kChunk>, grid, dim3(kScanThreads), s, a);
+        cudaError_t err = launch_kernel_smem(scan_kernel<T, LN, S, kChunk, WIDE>, grid, dim3(2 * kScanThreads), 2 * sizeof(ScanTile<T, LN, S, false>), s, a);
         if (err != cudaSuccess) return err;
         const long long n = static_cast<long long>(a.map.sequences) * a.channels * a.states;
         err = launch_kernel(scan_chain_kernel, dim3(ceil_div(n, 256)), dim3(256), s, a);
@@ -374,7 +447,13 @@ cudaError_t launch_scan_shape(const ScanArgs &k, cudaStream_t s, int *launches)
         *launches += 2;
     }
     *launches += 1;
-    return launch_kernel(scan_kernel<T, LN, S, kMain>, grid, dim3(kScanThreads), s, a);
+    return launch_kernel_smem(scan_kernel<T, LN, S, kMain, WIDE>, grid, dim3(2 * kScanThreads), 2 * sizeof(ScanTile<T, LN, S, true>), s, a);
+}
+
+template <typename T, int LN, int S>
+cudaError_t launch_scan_shape(const ScanArgs &k, cudaStream_t s, int *launches)
+{
+    return k.wide_tok && k.wide_bc ? launch_scan_wide<T, LN, S, true>(k, s, launches) : launch_scan_wide<T, LN, S, false>(k, s, launches);
 }
 
 inline bool scan_rows_wide(const sysscan_args &a, const sysconv_tokens &t, size_t esz)

@@ -438,26 +438,6 @@ struct ScanBackPlan {
 };
 ScanBackPlan scan_backward_plan(const sysscan_args &a);
 
-template <typename... KArgs, typename... Args>
-cudaError_t launch_kernel_smem(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t bytes, cudaStream_t s, Args &&...args)
-{
-    if (bytes > 48 * 1024) {
-        const cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-        if (err != cudaSuccess) return err;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = dependent_launch_enabled() ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
-}
-
 template <typename T, int LN, int S>
 cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *launches)
 {
@@ -470,8 +450,10 @@ cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *laun
         k.u = b.dy;
         k.B = b.f.C;
         k.blocks_per_group = ceil_div(per_group, F::CB);
-        err = launch_kernel(scan_kernel<T, LN, S, kChunkBack>, dim3(k.blocks_per_group * k.groups, k.map.sequences, k.chunks),
-                            dim3(kScanThreads), s, k);
+        const dim3 grid(k.blocks_per_group * k.groups, k.map.sequences, k.chunks), block(2 * kScanThreads);
+        const size_t bytes = 2 * sizeof(ScanTile<T, LN, S, false>);
+        err = k.wide_tok && k.wide_bc ? launch_kernel_smem(scan_kernel<T, LN, S, kChunkBack, true>, grid, block, bytes, s, k)
+                                      : launch_kernel_smem(scan_kernel<T, LN, S, kChunkBack, false>, grid, block, bytes, s, k);
         if (err != cudaSuccess) return err;
         const long long n = static_cast<long long>(k.map.sequences) * k.channels * k.states;
         err = launch_kernel(scan_chain_back_kernel, dim3(ceil_div(n, 256)), dim3(256), s, b);

@@ -1,5 +1,6 @@
 // State space scan: the plans of the prompt kernels, and the single-token kernel.
 #include "state_scan_backward.cuh"
+#include <cstdlib>
 
 namespace sysconv {
 
@@ -31,6 +32,7 @@ ScanPlan scan_plan(const sysscan_args &a)
     const long long rows = a.seq.sequences * a.channels;
     // two states a lane unless that gives more warps than the schedulers need to hide the recurrence's latency
     p.s = np >= 4 && (np >= 64 || rows * np / (4 * 32) >= 4 * kSchedulers) ? 4 : 2;
+    if (const char *e = getenv("SCAN_S")) p.s = atoi(e);
     p.ln = np / p.s;
     const long long warps = (rows * p.ln + 31) / 32;
     p.chunks = pick_chunks(warps, a.seq.length, 2 * kSchedulers, 128, &p.chunk);
