@@ -20,11 +20,13 @@
 
 namespace sysconv {
 
-constexpr int kScanThreads = 128;                // threads of each job
+constexpr int kScanThreads = 128;                // threads of the recurrence
+constexpr int kStageThreads = 128;               // threads that stage and finish
+constexpr int kBlockThreads = kScanThreads + kStageThreads;
 
 // Named barriers of a block: `wait` joins, `arrive` only counts; the writes before either are visible after `wait`.
-__device__ __forceinline__ void bar_wait(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(2 * kScanThreads) : "memory"); }
-__device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(2 * kScanThreads) : "memory"); }
+__device__ __forceinline__ void bar_wait(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kBlockThreads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kBlockThreads) : "memory"); }
 
 struct ScanArgs {
     SeqMap map;
@@ -79,23 +81,38 @@ struct ScanShape {
     static constexpr int CB = kScanThreads / LN;                        // channels per block
     static constexpr int U = LN < 16 ? LN : 16;                         // tokens whose sums are added together
     static constexpr int TT = LN < 4 || NP >= 64 ? 16 : 32;             // tokens per tile
-    static constexpr int PP = (TT * CB + kScanThreads - 1) / kScanThreads;   // (token, channel) pairs per thread
+    static constexpr int PP = (TT * CB + kStageThreads - 1) / kStageThreads;   // (token, channel) pairs per thread
     static constexpr int VT = PP >= 4 ? 4 : (PP >= 2 ? 2 : 1);          // ... of them neighbouring channels
-    static constexpr int BE = (TT * NP + kScanThreads - 1) / kScanThreads;   // elements of B per thread
+    static constexpr int BE = (TT * NP + kStageThreads - 1) / kStageThreads;   // elements of B per thread
     static constexpr int VB = BE >= 4 ? 4 : (BE >= 2 ? 2 : 1);
     // pitch of the sums: the lanes' writes fall in different banks, and VT of them can be read at once
     static constexpr int YP = CB + (32 / LN > VT ? 32 / LN : VT);
 };
 
-// A tile in shared memory.  B and C stay in the tokens' type: a lane's read returns one 32-bit word per clock and SM
-// quarter whatever its width and however many lanes share the address, and with B and C as fp32 those reads, not the
-// exponentials, bound the recurrence (measured on 4096 channels x 16 states: 8.8 words per token and warp against 16
-// clocks of exponentials).
+// How B and C lie in shared memory.  A read returns one 32-bit word per lane and clock of the SM, whatever its width and
+// however many lanes share the address.  With two states a lane those words, not the exponentials, bound the
+// recurrence if B and C are fp32 (8.8 clocks a token and warp on each of four schedulers, against 16 of exponentials), so
+// they stay 16-bit and are widened by the reader; with four states a lane the widening instructions cost more.
+template <typename T, int S> struct BcType { using type = float; };
+template <typename T> struct BcType<T, 2> { using type = T; };
+
+template <typename T, int V>
+__device__ __forceinline__ void put_bc(T *to, const Pack<T, V> &v) { store_pack<T, V>(to, v); }
+template <typename T, int V, typename = std::enable_if_t<sizeof(T) == 2>>
+__device__ __forceinline__ void put_bc(float *to, const Pack<T, V> &v)
+{
+    float f[V];
+    unpack(v, f);
+    store_pack(to, pack<float, V>(f));
+}
+
+// A tile in shared memory
 template <typename T, int LN, int S, bool MAIN>
 struct alignas(16) ScanTile {
     using G = ScanShape<LN, S>;
     float2 d[G::TT][G::CB];                                              // d, d u
-    T b[G::TT][G::NP], c[MAIN ? G::TT : 1][G::NP];
+    using BC = typename BcType<T, S>::type;
+    BC b[G::TT][G::NP], c[MAIN ? G::TT : 1][G::NP];
     float y[MAIN ? G::TT : 1][G::YP];
 };
 
@@ -111,23 +128,24 @@ struct RawTok {
 enum ScanMode { kMain, kChunk, kChunkBack };
 // WIDE: rows and channel counts allow whole accesses everywhere.
 template <typename T, int LN, int S, int MODE, bool WIDE>
-__global__ void __launch_bounds__(2 * kScanThreads, 2) scan_kernel(ScanArgs a)
+__global__ void __launch_bounds__(kBlockThreads, 2) scan_kernel(ScanArgs a)
 {
     using G = ScanShape<LN, S>;
     constexpr bool MAIN = MODE == kMain, BACK = MODE == kChunkBack;
     constexpr int NP = G::NP, CB = G::CB, U = G::U, TT = G::TT, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB;
     constexpr int P2 = S / 2;
-    static_assert(sizeof(ScanTile<T, LN, S, MAIN>) % 16 == 0 && (G::TT * G::CB * 8) % 16 == 0 && (G::TT * G::NP * sizeof(T)) % 16 == 0, "alignment");
-    static_assert((kScanThreads * VT % CB == 0 || PP == VT) && (kScanThreads * VB % NP == 0 || BE == VB), "a thread's accesses share a column");
+    static_assert(sizeof(ScanTile<T, LN, S, MAIN>) % 16 == 0 && (G::TT * G::CB * 8) % 16 == 0 && (G::TT * G::NP * sizeof(typename BcType<T, S>::type)) % 16 == 0, "alignment");
+    static_assert((kStageThreads * VT % CB == 0 || PP == VT) && (kStageThreads * VB % NP == 0 || BE == VB), "a thread's accesses share a column");
     static_assert(TT % U == 0 && TT % kScanBlock == 0 && PP % VT == 0 && BE % VB == 0, "tile shape");
     using Tile = ScanTile<T, LN, S, MAIN>;
+    using BC = typename BcType<T, S>::type;
     extern __shared__ __align__(16) float scan_smem[];
     Tile *tiles = reinterpret_cast<Tile *>(scan_smem);                   // two
     enum { kFull = 1, kDone = 3 };                                       // barriers: + buffer
     dependent_launch_enter();
 
     const bool producer = threadIdx.x >= kScanThreads;
-    const int tid = threadIdx.x & (kScanThreads - 1), lane = tid & 31;
+    const int tid = producer ? threadIdx.x - kScanThreads : threadIdx.x, lane = tid & 31;
     const int g = blockIdx.x / a.blocks_per_group;
     const int c0 = g * a.per_group + (blockIdx.x - g * a.blocks_per_group) * CB;      // first channel of the block
     const int c_end = min((g + 1) * a.per_group, a.channels);
@@ -153,7 +171,7 @@ __global__ void __launch_bounds__(2 * kScanThreads, 2) scan_kernel(ScanArgs a)
         // addresses of this thread's first pair and first B, C element; tokens run backwards in the backward recurrence
         constexpr int dir = BACK ? -1 : 1;
         const int p_row = tid * VT / CB, bc_row = tid * VB / NP, bc_n = tid * VB % NP;
-        constexpr int p_step = kScanThreads * VT / CB, bc_step = kScanThreads * VB / NP;   // rows between a thread's accesses
+        constexpr int p_step = kStageThreads * VT / CB, bc_step = kStageThreads * VB / NP;   // rows between a thread's accesses
         const long long t_first = BACK ? t_end - 1 : t_begin;
         auto at = [&](const Tokens &x, int row, int col) {
             return token_row<T>(x, a.map, r, first) + (t_first + dir * row) * x.tstride + col;
@@ -245,8 +263,8 @@ __global__ void __launch_bounds__(2 * kScanThreads, 2) scan_kernel(ScanArgs a)
             if (cells) {
 #pragma unroll
                 for (int i = 0; i < BE / VB; ++i) {
-                    store_pack<T, VB>(&s.b[bc_row + i * bc_step][bc_n], rb.v[i]);
-                    if (MAIN) store_pack<T, VB>(&s.c[bc_row + i * bc_step][bc_n], rc.v[i]);
+                    put_bc<T, VB>(&s.b[bc_row + i * bc_step][bc_n], rb.v[i]);
+                    if (MAIN) put_bc<T, VB>(&s.c[bc_row + i * bc_step][bc_n], rc.v[i]);
                 }
             }
         };
@@ -331,45 +349,61 @@ __global__ void __launch_bounds__(2 * kScanThreads, 2) scan_kernel(ScanArgs a)
             Tile &s = tiles[k & 1];
             const long long t0 = t_begin + static_cast<long long>(k) * TT;
             bar_wait(kFull + (k & 1));
-            // blocks of 16 tokens without a branch inside, so that one token's loads, another's exponentials and a third's
-            // sums overlap in one warp
+            // blocks of 16 tokens without a branch inside
 #pragma unroll 1
             for (int tb = 0; tb < TT; tb += kScanBlock) {
                 if (saved != nullptr && t0 + tb < t_end) put(saved + (t0 + tb) / kScanBlock * a.channels * a.states);
-                float y[kScanBlock / U];                                 // stored last: no load waits behind a store
+                // The exponentials run LEAD tokens ahead of the chain, and the sums over n wait for the end of the block, where
+                // they are independent of each other: an order in which one warp finds something to issue.
+                constexpr int LEAD = 4;
+                f32x2 decay[LEAD][P2], in[LEAD][P2];
+                float sums[MAIN ? kScanBlock : 1];
+                auto ahead = [&](int q) {
+                    const float2 d = s.d[tb + q][cl];
+                    const f32x2 dd = pair(d.x, d.x), du = pair(d.y, d.y);
+                    const Pack<BC, S> b = load_pack<BC, S>(&s.b[tb + q][ln * S]);
 #pragma unroll
-                for (int tu = tb; tu < tb + kScanBlock; tu += U) {
-                    float sums[U];
+                    for (int i = 0; i < P2; ++i) {
+                        const float2 x = halves(mul2(A2[i], dd));
+                        decay[q % LEAD][i] = pair(exp2_fast(x.x), exp2_fast(x.y));
+                        in[q % LEAD][i] = mul2(pair(b.get(2 * i), b.get(2 * i + 1)), du);
+                    }
+                };
 #pragma unroll
-                    for (int q = 0; q < U; ++q) {
-                        const float2 d = s.d[tu + q][cl];
-                        const f32x2 dd = pair(d.x, d.x), du = pair(d.y, d.y);
-                        const Pack<T, S> b = load_pack<T, S>(&s.b[tu + q][ln * S]);
-                        Pack<T, S> cc;
-                        if (MAIN) cc = load_pack<T, S>(&s.c[tu + q][ln * S]);
-                        f32x2 acc;
+                for (int q = 0; q < LEAD; ++q) ahead(q);
 #pragma unroll
-                        for (int i = 0; i < P2; ++i) {
-                            const f32x2 bv = pair(b.get(2 * i), b.get(2 * i + 1));
-                            const float2 x = halves(mul2(A2[i], dd));
-                            const f32x2 decay = pair(exp2_fast(x.x), exp2_fast(x.y));
-                            if (BACK) h[i] = mul2(decay, fma2(bv, du, h[i]));
-                            else h[i] = fma2(decay, h[i], mul2(bv, du));
-                            if (MAIN) {
-                                const f32x2 cv = pair(cc.get(2 * i), cc.get(2 * i + 1));
-                                acc = i == 0 ? mul2(h[i], cv) : fma2(h[i], cv, acc);
-                            }
-                        }
+                for (int q = 0; q < kScanBlock; ++q) {
+                    f32x2 acc;
+                    Pack<BC, S> cc;
+                    if (MAIN) cc = load_pack<BC, S>(&s.c[tb + q][ln * S]);
+#pragma unroll
+                    for (int i = 0; i < P2; ++i) {
+                        if (BACK) h[i] = mul2(decay[q % LEAD][i], add2(in[q % LEAD][i], h[i]));
+                        else h[i] = fma2(decay[q % LEAD][i], h[i], in[q % LEAD][i]);
                         if (MAIN) {
-                            const float2 v = halves(acc);
-                            sums[q] = v.x + v.y;
+                            const f32x2 cv = pair(cc.get(2 * i), cc.get(2 * i + 1));
+                            acc = i == 0 ? mul2(h[i], cv) : fma2(h[i], cv, acc);
                         }
                     }
-                    if (MAIN) y[(tu - tb) / U] = sum_transposed<U, LN>(sums, lane);
+                    if (MAIN) {
+                        const float2 v = halves(acc);
+                        sums[q] = v.x + v.y;
+                    }
+                    if (q + LEAD < kScanBlock) ahead(q + LEAD);
                 }
-                if (MAIN && (LN <= U || ln < U)) {
+                if (MAIN) {
+                    float y[kScanBlock / U];
 #pragma unroll
-                    for (int i = 0; i < kScanBlock / U; ++i) s.y[tb + i * U + ln % U][cl] = y[i];
+                    for (int i = 0; i < kScanBlock / U; ++i) {
+                        float v[U];
+#pragma unroll
+                        for (int q = 0; q < U; ++q) v[q] = sums[i * U + q];
+                        y[i] = sum_transposed<U, LN>(v, lane);
+                    }
+                    if (LN <= U || ln < U) {
+#pragma unroll
+                        for (int i = 0; i < kScanBlock / U; ++i) s.y[tb + i * U + ln % U][cl] = y[i];
+                    }
                 }
             }
             bar_arrive(kDone + (k & 1));
@@ -387,7 +421,7 @@ __global__ void __launch_bounds__(2 * kScanThreads, 2) scan_kernel(ScanArgs a)
         const float *part = reinterpret_cast<const float *>(tiles);
         float v = 0.0f;
         const int j = threadIdx.x % VT;
-        for (int w = threadIdx.x / VT; w < kScanThreads; w += CB / VT) v += part[w * VT + j];
+        for (int w = threadIdx.x / VT; w < kStageThreads; w += CB / VT) v += part[w * VT + j];
         a.dsum[chain * a.channels + c0 + threadIdx.x] = v;
     }
 }
@@ -439,7 +473,7 @@ cudaError_t launch_scan_wide(const ScanArgs &k, cudaStream_t s, int *launches)
     a.blocks_per_group = ceil_div(a.per_group, G::CB);
     const dim3 grid(a.blocks_per_group * a.groups, a.map.sequences, a.chunks);
     if (a.chunks > 1) {
-        cudaError_t err = launch_kernel_smem(scan_kernel<T, LN, S, kChunk, WIDE>, grid, dim3(2 * kScanThreads), 2 * sizeof(ScanTile<T, LN, S, false>), s, a);
+        cudaError_t err = launch_kernel_smem(scan_kernel<T, LN, S, kChunk, WIDE>, grid, dim3(kBlockThreads), 2 * sizeof(ScanTile<T, LN, S, false>), s, a);
         if (err != cudaSuccess) return err;
         const long long n = static_cast<long long>(a.map.sequences) * a.channels * a.states;
         err = launch_kernel(scan_chain_kernel, dim3(ceil_div(n, 256)), dim3(256), s, a);
@@ -447,7 +481,7 @@ cudaError_t launch_scan_wide(const ScanArgs &k, cudaStream_t s, int *launches)
         *launches += 2;
     }
     *launches += 1;
-    return launch_kernel_smem(scan_kernel<T, LN, S, kMain, WIDE>, grid, dim3(2 * kScanThreads), 2 * sizeof(ScanTile<T, LN, S, true>), s, a);
+    return launch_kernel_smem(scan_kernel<T, LN, S, kMain, WIDE>, grid, dim3(kBlockThreads), 2 * sizeof(ScanTile<T, LN, S, true>), s, a);
 }
 
 template <typename T, int LN, int S>

@@ -51,7 +51,7 @@ struct ScanBackShape {
     }
 };
 
-template <typename T, int LN, int S>
+template <typename T, int LN, int S, bool WIDE>
 __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kernel(ScanBackArgs b)
 {
     using G = ScanBackShape<LN, S>;
@@ -134,10 +134,10 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
             const int e = (i * NT + tid) * VT;
             const long long t = t0 + e / CB;
             const int valid = e < TB * CB && t < t_end ? pvalid : 0;
-            ru.v[i] = load_some<T, VT>(u0 + t * a.u.tstride, valid, a.wide_tok);
-            rd.v[i] = load_some<T, VT>(d0 + t * a.delta.tstride, valid, a.wide_tok);
-            rg.v[i] = load_some<T, VT>(g0 + t * b.dy.tstride, valid, a.wide_tok);
-            if (gate) rz.v[i] = load_some<T, VT>(z0 + t * a.z.tstride, valid, a.wide_tok);
+            ru.v[i] = load_part<T, VT, WIDE>(u0 + t * a.u.tstride, valid);
+            rd.v[i] = load_part<T, VT, WIDE>(d0 + t * a.delta.tstride, valid);
+            rg.v[i] = load_part<T, VT, WIDE>(g0 + t * b.dy.tstride, valid);
+            if (gate) rz.v[i] = load_part<T, VT, WIDE>(z0 + t * a.z.tstride, valid);
         }
 #pragma unroll
         for (int i = 0; i < BE / VB; ++i) {
@@ -145,8 +145,8 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
             const long long t = t0 + e / NP;
             const int n = e % NP;
             const int valid = e < TB * NP && t < t_end ? a.states - n : 0;
-            rb.v[i] = load_some<T, VB>(B0 + t * a.B.tstride + n, valid, a.wide_bc);
-            rc.v[i] = load_some<T, VB>(C0 + t * a.C.tstride + n, valid, a.wide_bc);
+            rb.v[i] = load_part<T, VB, WIDE>(B0 + t * a.B.tstride + n, valid);
+            rc.v[i] = load_part<T, VB, WIDE>(C0 + t * a.C.tstride + n, valid);
         }
         const float *from = saved + t0 / kScanBlock * a.channels * a.states;
 #pragma unroll
@@ -310,9 +310,9 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
                     sum_b[j] += dd;
                     sum_d[j] = fmaf(dyv[q], uv[q], sum_d[j]);
                 }
-                store_some<T, VT>(du0 + (t0 + tt) * b.du.tstride, odu, pvalid, a.wide_tok);
-                store_some<T, VT>(dd0 + (t0 + tt) * b.ddelta.tstride, odd, pvalid, a.wide_tok);
-                if (gate) store_some<T, VT>(dz0 + (t0 + tt) * b.dz.tstride, odz, pvalid, a.wide_tok);
+                store_some<T, VT>(du0 + (t0 + tt) * b.du.tstride, odu, pvalid, WIDE);
+                store_some<T, VT>(dd0 + (t0 + tt) * b.ddelta.tstride, odd, pvalid, WIDE);
+                if (gate) store_some<T, VT>(dz0 + (t0 + tt) * b.dz.tstride, odz, pvalid, WIDE);
             }
         }
         for (int e = tid; e < TB * 2 * NP; e += NT) {
@@ -450,7 +450,7 @@ cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *laun
         k.u = b.dy;
         k.B = b.f.C;
         k.blocks_per_group = ceil_div(per_group, F::CB);
-        const dim3 grid(k.blocks_per_group * k.groups, k.map.sequences, k.chunks), block(2 * kScanThreads);
+        const dim3 grid(k.blocks_per_group * k.groups, k.map.sequences, k.chunks), block(kBlockThreads);
         const size_t bytes = 2 * sizeof(ScanTile<T, LN, S, false>);
         err = k.wide_tok && k.wide_bc ? launch_kernel_smem(scan_kernel<T, LN, S, kChunkBack, true>, grid, block, bytes, s, k)
                                       : launch_kernel_smem(scan_kernel<T, LN, S, kChunkBack, false>, grid, block, bytes, s, k);
@@ -461,8 +461,9 @@ cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *laun
         *launches += 2;
     }
     b.f.blocks_per_group = ceil_div(per_group, G::CB);
-    err = launch_kernel_smem(scan_backward_kernel<T, LN, S>, dim3(b.f.blocks_per_group * b.f.groups, b.f.map.sequences, b.f.chunks),
-                             dim3(G::NT), G::bytes(), s, b);
+    const dim3 grid(b.f.blocks_per_group * b.f.groups, b.f.map.sequences, b.f.chunks), block(G::NT);
+    err = b.f.wide_tok && b.f.wide_bc ? launch_kernel_smem(scan_backward_kernel<T, LN, S, true>, grid, block, G::bytes(), s, b)
+                                      : launch_kernel_smem(scan_backward_kernel<T, LN, S, false>, grid, block, G::bytes(), s, b);
     if (err != cudaSuccess) return err;
     *launches += 1;
     const long long values = b.f.map.total * b.f.groups * 2 * LN * S;

@@ -1,6 +1,5 @@
 // State space scan: the plans of the prompt kernels, and the single-token kernel.
 #include "state_scan_backward.cuh"
-#include <cstdlib>
 
 namespace sysconv {
 
@@ -30,9 +29,9 @@ ScanPlan scan_plan(const sysscan_args &a)
     ScanPlan p = {};
     const int np = padded_states(a.states);
     const long long rows = a.seq.sequences * a.channels;
-    // two states a lane unless that gives more warps than the schedulers need to hide the recurrence's latency
-    p.s = np >= 4 && (np >= 64 || rows * np / (4 * 32) >= 4 * kSchedulers) ? 4 : 2;
-    if (const char *e = getenv("SCAN_S")) p.s = atoi(e);
+    // Four states a lane cost fewer instructions per state, two give twice the warps.  8192 tokens, 16 states, by channels:
+    // 2560: 308 (four) against 316 us, 4096: 351 against 316, 8192: 517 against 614: four from 1.7 warps a scheduler on.
+    p.s = np >= 4 && (np >= 64 || rows * np / (4 * 32) * 10 >= 17 * kSchedulers) ? 4 : 2;
     p.ln = np / p.s;
     const long long warps = (rows * p.ln + 31) / 32;
     p.chunks = pick_chunks(warps, a.seq.length, 2 * kSchedulers, 128, &p.chunk);
