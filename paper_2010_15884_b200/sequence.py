@@ -66,31 +66,29 @@ def _bytes(size, where):
     return size
 
 
-class _on:
-    """The device of x and the stream of the call made current; costs nothing where they already are."""
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_packed_rows = torch.contiguous_format
 
-    __slots__ = ("stack", "stream")
 
-    def __init__(self, x, stream, where):
-        if not x.is_cuda:
-            raise SysconvError(-1, "%s (not a CUDA tensor; there is no CPU path)" % where)
-        self.stack = None
-        if stream is not None or x.device.index != torch.cuda.current_device():
-            self.stack = contextlib.ExitStack()
-            self.stack.enter_context(torch.cuda.device(x.device))
-            if stream is not None:
-                if isinstance(stream, int):
-                    stream = torch.cuda.ExternalStream(stream, device=x.device)
-                self.stack.enter_context(torch.cuda.stream(stream))
-        self.stream = torch._C._cuda_getCurrentRawStream(x.device.index)
+@contextlib.contextmanager
+def _there(x, stream, where):
+    """The device of x and the stream of the call made current."""
+    if not x.is_cuda:
+        raise SysconvError(-1, "%s (not a CUDA tensor; there is no CPU path)" % where)
+    with torch.cuda.device(x.device):
+        if stream is None:
+            yield
+        else:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=x.device)
+            with torch.cuda.stream(stream):
+                yield
 
-    def __enter__(self):
-        return self.stream
 
-    def __exit__(self, *exc):
-        if self.stack is not None:
-            self.stack.close()
-        return False
+def _elsewhere(x, stream):
+    """Whether the call has to change device or stream first (or has no device at all)."""
+    return stream is not None or not x.is_cuda or x.get_device() != _device()
 
 
 def _type(x):
@@ -107,32 +105,31 @@ def _act(activation):
     return a
 
 
-def _tok(x, name, like, channels_like=True):
-    """(pointer, batch stride, time stride) of a token tensor with the type, device and leading sizes of `like`."""
-    if x.dtype != like.dtype or x.device != like.device:
+def _tok(x, name, like, shape):
+    """(pointer, batch stride, time stride) of a token tensor of the type and device of `like`."""
+    if x.dtype is not like.dtype or x.get_device() != like.get_device():
         raise TypeError("%s: type and device must be those of the tokens (%s on %s), got %s on %s"
                         % (name, like.dtype, like.device, x.dtype, x.device))
-    shape, want = x.shape, like.shape
-    if (shape != want) if channels_like else (shape[: len(want) - 1] != want[:-1]):
-        raise ValueError("%s: shape %s does not go with tokens %s" % (name, tuple(shape), tuple(want)))
+    if x.shape != shape:
+        raise ValueError("%s: shape %s where %s is wanted" % (name, tuple(x.shape), tuple(shape)))
     s = x.stride()
     if s[-1] != 1 and shape[-1] > 1 and x.numel() > 0:
         raise ValueError("%s: channels must be contiguous" % name)
-    if len(want) == 3:
+    if len(s) == 3:
         return x.data_ptr(), s[0], s[1]
     return x.data_ptr(), 0, s[0]
 
 
-def _par(x, name, shape, dtype, device, optional=True):
-    """Pointer of a packed parameter; 0 for None."""
+def _par(x, name, shape, dtype, like, optional=True):
+    """Pointer of a packed parameter on the device of `like`; 0 for None."""
     if x is None:
         if optional:
             return 0
         raise ValueError("%s is needed" % name)
-    if x.dtype != dtype or x.device != device:
-        raise TypeError("%s must be %s on %s, got %s on %s" % (name, dtype, device, x.dtype, x.device))
-    if tuple(x.shape) != shape:
-        raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(x.shape)))
+    if x.dtype is not dtype or x.get_device() != like.get_device():
+        raise TypeError("%s must be %s on %s, got %s on %s" % (name, dtype, like.device, x.dtype, x.device))
+    if x.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return x.data_ptr()
@@ -141,9 +138,10 @@ def _par(x, name, shape, dtype, device, optional=True):
 def _sequences(x, offsets, longest=None):
     """((sequences, length, total, offsets pointer, 64-bit), sequences) of a token tensor."""
     if offsets is None:
-        if x.dim() != 3:
+        shape = x.shape
+        if len(shape) != 3:
             raise ValueError("dense tokens are (batch, length, channels); packed ones need offsets")
-        b, n, _ = x.shape
+        b, n, _ = shape
         return (b, n, b * n, 0, 0), b
     if x.dim() != 2:
         raise ValueError("packed tokens are (tokens, channels)")
@@ -156,33 +154,30 @@ def _sequences(x, offsets, longest=None):
     return (r, max(most, 0), total, offsets.data_ptr(), 1 if offsets.dtype == torch.int64 else 0), r
 
 
-def _slots(slots, rows, device):
+def _slots(slots, rows, like):
     if slots is None:
         return 0
-    if slots.dtype != torch.int32 or slots.device != device or slots.dim() != 1 or slots.shape[0] != rows or not slots.is_contiguous():
+    if slots.dtype is not torch.int32 or slots.get_device() != like.get_device() or slots.shape != (rows,) or not slots.is_contiguous():
         raise ValueError("slots: a contiguous int32 vector with one slot per row, on the tokens' device")
     return slots.data_ptr()
 
 
-def _room(size, device):
+def _room(size, like):
     """A workspace of `size` bytes."""
-    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    return torch.empty(size, dtype=torch.uint8, device=like.device) if size else None
 
 
 # ---------------------------------------------------------------------------------------------- causal convolution
 
 
-def _causal_params(x, weight, bias):
-    if weight.dim() != 2 or weight.shape[0] != x.shape[-1]:
-        raise ValueError("weight must be (channels, taps), got %s for %d channels" % (tuple(weight.shape), x.shape[-1]))
-    if weight.dtype != x.dtype and weight.dtype != torch.float32:
+def _causal_params(x, d, weight, bias):
+    """(taps, weight pointer, bias pointer, weight type)"""
+    shape, kind = weight.shape, weight.dtype
+    if len(shape) != 2 or shape[0] != d or shape[1] < 1:
+        raise ValueError("weight must be (channels, taps), got %s for %d channels" % (tuple(shape), d))
+    if kind is not x.dtype and kind is not torch.float32:
         raise TypeError("weight must be float32 or of the tokens' type")
-    d, k = weight.shape
-    if k < 1:
-        raise ValueError("weight has no taps")
-    w = _par(weight, "weight", (d, k), weight.dtype, x.device)
-    b = _par(bias, "bias", (d,), weight.dtype, x.device)
-    return d, k, w, b, _TYPES[weight.dtype]
+    return shape[1], _par(weight, "weight", shape, kind, x), _par(bias, "bias", (d,), kind, x), _TYPES[kind]
 
 
 def conv1d_causal(x, weight, bias=None, activation=None, state=None, offsets=None, return_state=False, out=None, stream=None):
@@ -191,18 +186,21 @@ def conv1d_causal(x, weight, bias=None, activation=None, state=None, offsets=Non
     weight (channels, taps), taps <= 8; bias (channels); both float32 or of x's type.  state (sequences, taps-1, channels) of
     x's type: the inputs before the first token (zeros without it).  Returns y, or (y, final state) with return_state.
     """
-    with _on(x, stream, "conv1d_causal") as s:
-        t, act = _type(x), _act(activation)
-        seq, r = _sequences(x, offsets)
-        d, k, w, b, wt = _causal_params(x, weight, bias)
-        st = _par(state, "state", (r, k - 1, d), x.dtype, x.device)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        final = torch.empty((r, k - 1, d), dtype=x.dtype, device=x.device) if return_state else None
-        if r > 0 and d > 0:
-            args = _CAUSAL.pack(*seq, d, k, t, wt, act, *_tok(x, "x", x), *_tok(y, "out", x), *_NONE3, w, b, st,
-                                final.data_ptr() if final is not None else 0, 0, 0, 0, 0, 0, 0)
-            _check(_library().sysconv1d_causal(args, s), "sysconv1d_causal")
-        return (y, final) if return_state else y
+    if _elsewhere(x, stream):
+        with _there(x, stream, "conv1d_causal"):
+            return conv1d_causal(x, weight, bias, activation, state, offsets, return_state, out)
+    t, act, shape = _type(x), _act(activation), x.shape
+    seq, r = _sequences(x, offsets)
+    d = shape[-1]
+    k, w, b, wt = _causal_params(x, d, weight, bias)
+    st = _par(state, "state", (r, k - 1, d), x.dtype, x)
+    y = torch.empty_like(x, memory_format=_packed_rows) if out is None else out
+    final = x.new_empty((r, k - 1, d)) if return_state else None
+    if r > 0 and d > 0:
+        args = _CAUSAL.pack(*seq, d, k, t, wt, act, *_tok(x, "x", x, shape), *_tok(y, "out", x, shape), *_NONE3, w, b, st,
+                            final.data_ptr() if return_state else 0, 0, 0, 0, 0, 0, 0)
+        _check(_library().sysconv1d_causal(args, _raw_stream(x.get_device())), "sysconv1d_causal")
+    return (y, final) if return_state else y
 
 
 def conv1d_causal_backward(dy, x, weight, bias=None, activation=None, state=None, offsets=None, dfinal=None, stream=None):
@@ -210,26 +208,29 @@ def conv1d_causal_backward(dy, x, weight, bias=None, activation=None, state=None
 
     dfinal: gradient with respect to the final state, if that was used.
     """
-    with _on(x, stream, "conv1d_causal_backward") as s:
-        t, act = _type(x), _act(activation)
-        seq, r = _sequences(x, offsets)
-        d, k, w, b, wt = _causal_params(x, weight, bias)
-        st = _par(state, "state", (r, k - 1, d), x.dtype, x.device)
-        df = _par(dfinal, "dfinal", (r, k - 1, d), x.dtype, x.device)
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dw = torch.empty_like(weight)
-        db = torch.empty_like(bias) if bias is not None else None
-        ds = torch.empty_like(state) if state is not None else None
-        if r == 0 or d == 0:
-            return dx, dw.zero_(), db.zero_() if db is not None else None, ds
-        head = (*seq, d, k, t, wt, act, *_tok(x, "x", x), *_tok(dy, "dy", x), *_tok(dx, "dx", x), w, b, st, 0, df,
-                ds.data_ptr() if ds is not None else 0, dw.data_ptr(), db.data_ptr() if db is not None else 0)
-        lib = _library()
-        size = _bytes(lib.sysconv1d_causal_backward_workspace_bytes(_CAUSAL.pack(*head, 0, 0)), "sysconv1d_causal_backward")
-        room = _room(size, x.device)
-        args = _CAUSAL.pack(*head, room.data_ptr() if room is not None else 0, size)
-        _check(lib.sysconv1d_causal_backward(args, s), "sysconv1d_causal_backward")
-        return dx, dw, db, ds
+    if _elsewhere(x, stream):
+        with _there(x, stream, "conv1d_causal_backward"):
+            return conv1d_causal_backward(dy, x, weight, bias, activation, state, offsets, dfinal)
+    t, act, shape = _type(x), _act(activation), x.shape
+    seq, r = _sequences(x, offsets)
+    d = shape[-1]
+    k, w, b, wt = _causal_params(x, d, weight, bias)
+    st = _par(state, "state", (r, k - 1, d), x.dtype, x)
+    df = _par(dfinal, "dfinal", (r, k - 1, d), x.dtype, x)
+    dx = torch.empty_like(x, memory_format=_packed_rows)
+    dw = torch.empty_like(weight)
+    db = torch.empty_like(bias) if bias is not None else None
+    ds = torch.empty_like(state) if state is not None else None
+    if r == 0 or d == 0:
+        return dx, dw.zero_(), db.zero_() if db is not None else None, ds
+    head = (*seq, d, k, t, wt, act, *_tok(x, "x", x, shape), *_tok(dy, "dy", x, shape), *_tok(dx, "dx", x, shape), w, b, st, 0, df,
+            _ptr(ds), dw.data_ptr(), _ptr(db))
+    lib = _library()
+    size = _bytes(lib.sysconv1d_causal_backward_workspace_bytes(_CAUSAL.pack(*head, 0, 0)), "sysconv1d_causal_backward")
+    room = _room(size, x)
+    args = _CAUSAL.pack(*head, _ptr(room), size)
+    _check(lib.sysconv1d_causal_backward(args, _raw_stream(x.get_device())), "sysconv1d_causal_backward")
+    return dx, dw, db, ds
 
 
 def conv1d_causal_step(x, state, weight, bias=None, activation=None, slots=None, out=None, stream=None):
@@ -238,75 +239,83 @@ def conv1d_causal_step(x, state, weight, bias=None, activation=None, slots=None,
     slots (int32, one per row): the slot of each row; a slot outside the cache (-1, say) gives zeros and touches no
     state.  Without it row r uses slot r.  No two rows may name the same slot.
     """
-    with _on(x, stream, "conv1d_causal_step") as s:
-        t, act = _type(x), _act(activation)
-        if x.dim() != 2:
-            raise ValueError("x must be (rows, channels)")
-        rows = x.shape[0]
-        d, k, w, b, wt = _causal_params(x, weight, bias)
-        n = _cache(state, (k - 1, d), x.dtype, x.device)
-        at = _slots(slots, rows, x.device)
-        if slots is None and n < rows:
-            raise ValueError("state has %d slots for %d rows" % (n, rows))
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        xp, _, xs = _tok(x, "x", x)
-        yp, _, ys = _tok(y, "out", x)
-        if rows > 0 and d > 0:
-            args = _CAUSAL_STEP.pack(rows, n, d, k, t, wt, act, xp, xs, yp, ys, state.data_ptr(), state.stride(0), w, b, at)
-            _check(_library().sysconv1d_causal_step(args, s), "sysconv1d_causal_step")
-        return y
+    if _elsewhere(x, stream):
+        with _there(x, stream, "conv1d_causal_step"):
+            return conv1d_causal_step(x, state, weight, bias, activation, slots, out)
+    t, act, shape = _type(x), _act(activation), x.shape
+    if len(shape) != 2:
+        raise ValueError("x must be (rows, channels)")
+    rows, d = shape
+    k, w, b, wt = _causal_params(x, d, weight, bias)
+    n = _cache(state, k - 1, d, x.dtype, x)
+    at = _slots(slots, rows, x)
+    if slots is None and n < rows:
+        raise ValueError("state has %d slots for %d rows" % (n, rows))
+    y = torch.empty_like(x, memory_format=_packed_rows) if out is None else out
+    xp, _, xs = _tok(x, "x", x, shape)
+    yp, _, ys = _tok(y, "out", x, shape)
+    if rows > 0 and d > 0:
+        args = _CAUSAL_STEP.pack(rows, n, d, k, t, wt, act, xp, xs, yp, ys, state.data_ptr(), state.stride(0), w, b, at)
+        _check(_library().sysconv1d_causal_step(args, _raw_stream(x.get_device())), "sysconv1d_causal_step")
+    return y
 
 
-def _cache(state, shape, dtype, device):
-    """Slots of a cache of states: each slot packed, any stride between them."""
-    if state.dtype != dtype or state.device != device:
-        raise TypeError("state must be %s on %s, got %s on %s" % (dtype, device, state.dtype, state.device))
-    if state.dim() != 3 or tuple(state.shape[1:]) != shape:
-        raise ValueError("state must be (slots, %d, %d), got %s" % (shape[0], shape[1], tuple(state.shape)))
+def _ptr(x):
+    return 0 if x is None else x.data_ptr()
+
+
+def _cache(state, a, b, dtype, like):
+    """Number of slots of a cache of (a, b) states: each slot packed, any stride between them."""
+    if state.dtype is not dtype or state.get_device() != like.get_device():
+        raise TypeError("state must be %s on %s, got %s on %s" % (dtype, like.device, state.dtype, state.device))
+    shape = state.shape
+    if len(shape) != 3 or shape[1] != a or shape[2] != b:
+        raise ValueError("state must be (slots, %d, %d), got %s" % (a, b, tuple(shape)))
     s = state.stride()
-    if state.numel() > 0 and ((shape[1] > 1 and s[2] != 1) or (shape[0] > 1 and s[1] != shape[1])):
+    if ((b > 1 and s[2] != 1) or (a > 1 and s[1] != b)) and state.numel() > 0:
         raise ValueError("each slot of state must be contiguous")
-    return state.shape[0]
+    return shape[0]
 
 
 # ---------------------------------------------------------------------------------------------- state space scan
 
 
-def _scan_shapes(u, A, B, C):
+def _scan_shapes(u, lead, A, B, C):
+    """(states, groups) of a scan over tokens with the leading sizes `lead`."""
     d = u.shape[-1]
-    if A.dim() != 2 or A.shape[0] != d:
-        raise ValueError("A must be (channels, states), got %s for %d channels" % (tuple(A.shape), d))
-    n, lead = A.shape[1], u.dim() - 1
-    if B.dim() == lead + 1:
-        g = 1
-    elif B.dim() == lead + 2:
-        g = B.shape[lead]
-    else:
-        raise ValueError("B and C must be (..., states) or (..., groups, states)")
-    if B.shape != C.shape or B.shape[-1] != n or B.shape[:lead] != u.shape[:-1]:
-        raise ValueError("B %s and C %s do not go with tokens %s and %d states"
-                         % (tuple(B.shape), tuple(C.shape), tuple(u.shape), n))
+    a, shape = A.shape, B.shape
+    if len(a) != 2 or a[0] != d:
+        raise ValueError("A must be (channels, states), got %s for %d channels" % (tuple(a), d))
+    n, k = a[1], len(lead)
+    if shape != C.shape or len(shape) not in (k + 1, k + 2) or shape[-1] != n or shape[:k] != lead:
+        raise ValueError("B %s and C %s must be (..., states) or (..., groups, states) for tokens %s and %d states"
+                         % (tuple(shape), tuple(C.shape), tuple(u.shape), n))
+    g = 1 if len(shape) == k + 1 else shape[k]
     if g < 1 or d % g != 0:
         raise ValueError("%d channels do not divide into %d groups" % (d, g))
-    return d, n, g
+    return n, g
 
 
-def _bc(x, name, u, n, g):
-    """B or C: like tokens, the groups' states packed within a token."""
-    if x.dim() == u.dim() + 1 and g > 1 and x.stride(-2) != n:
-        raise ValueError("%s: the groups of a token must be contiguous" % name)
-    return _tok(x, name, u, channels_like=False)
+def _bc(x, name, u, n, g, k):
+    """(pointer, batch stride, time stride) of B or C, whose groups are packed within a token; k leading sizes."""
+    if x.dtype is not u.dtype or x.get_device() != u.get_device():
+        raise TypeError("%s: type and device must be those of the tokens (%s on %s), got %s on %s"
+                        % (name, u.dtype, u.device, x.dtype, x.device))
+    s = x.stride()
+    if ((s[-1] != 1 and n > 1) or (g > 1 and s[-2] != n)) and x.numel() > 0:
+        raise ValueError("%s: the states and groups of a token must be contiguous" % name)
+    return (x.data_ptr(), s[0], s[1]) if k == 2 else (x.data_ptr(), 0, s[0])
 
 
 def _scan_head(u, delta, A, B, C, D, z, delta_bias, softplus, offsets, longest):
-    t = _type(u)
+    t, shape = _type(u), u.shape
     seq, r = _sequences(u, offsets, longest)
-    d, n, g = _scan_shapes(u, A, B, C)
-    f32, dev = torch.float32, u.device
-    head = (*seq, d, n, g, t, 1 if softplus else 0, *_tok(u, "u", u), *_tok(delta, "delta", u),
-            *(_tok(z, "z", u) if z is not None else _NONE3), *_bc(B, "B", u, n, g), *_bc(C, "C", u, n, g))
-    params = (_par(A, "A", (d, n), f32, dev, False), _par(D, "D", (d,), f32, dev),
-              _par(delta_bias, "delta_bias", (d,), f32, dev))
+    d, lead = shape[-1], shape[:-1]
+    n, g = _scan_shapes(u, lead, A, B, C)
+    f32, k = torch.float32, len(lead)
+    head = (*seq, d, n, g, t, 1 if softplus else 0, *_tok(u, "u", u, shape), *_tok(delta, "delta", u, shape),
+            *(_tok(z, "z", u, shape) if z is not None else _NONE3), *_bc(B, "B", u, n, g, k), *_bc(C, "C", u, n, g, k))
+    params = (_par(A, "A", A.shape, f32, u, False), _par(D, "D", (d,), f32, u), _par(delta_bias, "delta_bias", (d,), f32, u))
     return head, params, r, d, n, g
 
 
@@ -319,29 +328,28 @@ def state_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=Fals
     (sequences, channels, states): float32.  states <= 128.
     Returns y; with return_state also the final state, with save also what state_scan_backward needs, in this order.
     """
-    with _on(u, stream, "state_scan") as s:
-        head, params, r, d, n, g = _scan_head(u, delta, A, B, C, D, z, delta_bias, softplus, offsets, longest)
-        dev, f32 = u.device, torch.float32
-        st = _par(state, "state", (r, d, n), f32, dev)
-        y = torch.empty(u.shape, dtype=u.dtype, device=dev) if out is None else out
-        yt = _tok(y, "out", u)
-        final = torch.empty((r, d, n), dtype=f32, device=dev) if return_state else None
-        lib, saved = _library(), None
-        fp = final.data_ptr() if final is not None else 0
-        body, rest = (*head, *yt, *params, st, fp), _NONE3 * 6 + (0,) * 5     # rest: the backward call's members
-        args = _SCAN.pack(*body, 0, *rest, 0, 0)
-        if save:
-            blocks = lib.sysscan_saved_blocks(args) if r > 0 else 0
-            saved = torch.empty((max(blocks, 0), d, n), dtype=f32, device=dev)
-        if r > 0 and d > 0:
-            size = _bytes(lib.sysscan_workspace_bytes(args), "sysscan")
-            if size or save:
-                room = _room(size, dev)
-                args = _SCAN.pack(*body, saved.data_ptr() if save else 0, *rest, room.data_ptr() if size else 0, size)
-            _check(lib.sysscan(args, s), "sysscan")
-        if not return_state and not save:
-            return y
-        return (y,) + ((final,) if return_state else ()) + ((saved,) if save else ())
+    if _elsewhere(u, stream):
+        with _there(u, stream, "state_scan"):
+            return state_scan(u, delta, A, B, C, D, z, delta_bias, softplus, state, offsets, longest, return_state, save, out)
+    head, params, r, d, n, g = _scan_head(u, delta, A, B, C, D, z, delta_bias, softplus, offsets, longest)
+    st = _par(state, "state", (r, d, n), torch.float32, u)
+    y = torch.empty_like(u, memory_format=_packed_rows) if out is None else out
+    final = A.new_empty((r, d, n)) if return_state else None
+    lib, saved = _library(), None
+    body = (*head, *_tok(y, "out", u, u.shape), *params, st, _ptr(final))
+    rest = _NONE3 * 6 + (0,) * 5                                          # the backward call's members
+    args = _SCAN.pack(*body, 0, *rest, 0, 0)
+    if save:
+        saved = A.new_empty((lib.sysscan_saved_blocks(args) if r > 0 else 0, d, n))
+    if r > 0 and d > 0:
+        size = _bytes(lib.sysscan_workspace_bytes(args), "sysscan")
+        if size or save:
+            room = _room(size, u)
+            args = _SCAN.pack(*body, _ptr(saved), *rest, _ptr(room), size)
+        _check(lib.sysscan(args, _raw_stream(u.get_device())), "sysscan")
+    if not return_state and not save:
+        return y
+    return (y,) + ((final,) if return_state else ()) + ((saved,) if save else ())
 
 
 def state_scan_backward(dy, u, delta, A, B, C, saved, D=None, z=None, delta_bias=None, softplus=False, offsets=None,
@@ -351,68 +359,65 @@ def state_scan_backward(dy, u, delta, A, B, C, saved, D=None, z=None, delta_bias
     dfinal: gradient with respect to the final state, if that was used.  dz, dD, ddelta_bias are None where z, D, delta_bias
     are; dstate (the gradient with respect to the initial state) is computed on state_grad.
     """
-    with _on(u, stream, "state_scan_backward") as s:
-        head, params, r, d, n, g = _scan_head(u, delta, A, B, C, D, z, delta_bias, softplus, offsets, longest)
-        dev, f32 = u.device, torch.float32
-        df = _par(dfinal, "dfinal", (r, d, n), f32, dev)
-        du = torch.empty(u.shape, dtype=u.dtype, device=dev)
-        dd = torch.empty(u.shape, dtype=u.dtype, device=dev)
-        dz = torch.empty(u.shape, dtype=u.dtype, device=dev) if z is not None else None
-        dB = torch.empty(B.shape, dtype=B.dtype, device=dev)
-        dC = torch.empty(C.shape, dtype=C.dtype, device=dev)
-        dA = torch.empty((d, n), dtype=f32, device=dev)
-        dD = torch.empty(d, dtype=f32, device=dev) if D is not None else None
-        dbias = torch.empty(d, dtype=f32, device=dev) if delta_bias is not None else None
-        dstate = torch.empty((r, d, n), dtype=f32, device=dev) if state_grad else None
-        if r == 0 or d == 0:
-            dA.zero_()
-            for v in (dD, dbias):
-                if v is not None:
-                    v.zero_()
-            return ScanGrads(du, dd, dA, dB, dC, dD, dz, dbias, dstate)
-
-        def ptr(v):
-            return v.data_ptr() if v is not None else 0
-
-        lib = _library()
-        probe = _SCAN.pack(*head, *_NONE3, *params, 0, 0, 0, *_NONE3 * 6, 0, 0, 0, 0, 0, 0, 0)
-        blocks = lib.sysscan_saved_blocks(probe)
-        _par(saved, "saved", (blocks, d, n), f32, dev, False)
-        body = (*head, *_NONE3, *params, 0, 0, ptr(saved), *_tok(dy, "dy", u), *_tok(du, "du", u), *_tok(dd, "ddelta", u),
-                *(_tok(dz, "dz", u) if dz is not None else _NONE3), *_bc(dB, "dB", u, n, g), *_bc(dC, "dC", u, n, g),
-                ptr(dA), ptr(dD), ptr(dbias), df, ptr(dstate))
-        size = _bytes(lib.sysscan_backward_workspace_bytes(_SCAN.pack(*body, 0, 0)), "sysscan_backward")
-        room = _room(size, dev)
-        _check(lib.sysscan_backward(_SCAN.pack(*body, ptr(room), size), s), "sysscan_backward")
+    if _elsewhere(u, stream):
+        with _there(u, stream, "state_scan_backward"):
+            return state_scan_backward(dy, u, delta, A, B, C, saved, D, z, delta_bias, softplus, offsets, longest, dfinal, state_grad)
+    head, params, r, d, n, g = _scan_head(u, delta, A, B, C, D, z, delta_bias, softplus, offsets, longest)
+    f32, shape, k = torch.float32, u.shape, u.dim() - 1
+    df = _par(dfinal, "dfinal", (r, d, n), f32, u)
+    du, dd = (torch.empty_like(u, memory_format=_packed_rows) for _ in range(2))
+    dz = torch.empty_like(u, memory_format=_packed_rows) if z is not None else None
+    dB, dC = (torch.empty_like(B, memory_format=_packed_rows) for _ in range(2))
+    dA = torch.empty_like(A)
+    dD = torch.empty_like(D) if D is not None else None
+    dbias = torch.empty_like(delta_bias) if delta_bias is not None else None
+    dstate = A.new_empty((r, d, n)) if state_grad else None
+    if r == 0 or d == 0:
+        dA.zero_()
+        for v in (dD, dbias):
+            if v is not None:
+                v.zero_()
         return ScanGrads(du, dd, dA, dB, dC, dD, dz, dbias, dstate)
+    lib = _library()
+    blocks = lib.sysscan_saved_blocks(_SCAN.pack(*head, *_NONE3, *params, 0, 0, 0, *_NONE3 * 6, 0, 0, 0, 0, 0, 0, 0))
+    body = (*head, *_NONE3, *params, 0, 0, _par(saved, "saved", (blocks, d, n), f32, u, False), *_tok(dy, "dy", u, shape),
+            *_tok(du, "du", u, shape), *_tok(dd, "ddelta", u, shape), *(_tok(dz, "dz", u, shape) if z is not None else _NONE3),
+            *_bc(dB, "dB", u, n, g, k), *_bc(dC, "dC", u, n, g, k), dA.data_ptr(), _ptr(dD), _ptr(dbias), df, _ptr(dstate))
+    size = _bytes(lib.sysscan_backward_workspace_bytes(_SCAN.pack(*body, 0, 0)), "sysscan_backward")
+    room = _room(size, u)
+    _check(lib.sysscan_backward(_SCAN.pack(*body, _ptr(room), size), _raw_stream(u.get_device())), "sysscan_backward")
+    return ScanGrads(du, dd, dA, dB, dC, dD, dz, dbias, dstate)
 
 
 def state_scan_step(u, delta, A, B, C, state, D=None, z=None, delta_bias=None, softplus=False, slots=None, out=None, stream=None):
     """One token of each row: u, delta, z (rows, channels), B, C (rows[, groups], states); state (slots, channels, states),
     float32, is updated in place.  Slots as in conv1d_causal_step.  Returns y."""
-    with _on(u, stream, "state_scan_step") as s:
-        t = _type(u)
-        if u.dim() != 2:
-            raise ValueError("u must be (rows, channels)")
-        d, n, g = _scan_shapes(u, A, B, C)
-        rows, f32, dev = u.shape[0], torch.float32, u.device
-        slots_n = _cache(state, (d, n), f32, dev)
-        at = _slots(slots, rows, dev)
-        if slots is None and slots_n < rows:
-            raise ValueError("state has %d slots for %d rows" % (slots_n, rows))
-        y = torch.empty(u.shape, dtype=u.dtype, device=dev) if out is None else out
-        up, _, us = _tok(u, "u", u)
-        dp, _, ds = _tok(delta, "delta", u)
-        zp, _, zs = _tok(z, "z", u) if z is not None else _NONE3
-        bp, _, bs = _bc(B, "B", u, n, g)
-        cp, _, cs = _bc(C, "C", u, n, g)
-        yp, _, ys = _tok(y, "out", u)
-        if rows > 0 and d > 0:
-            args = _SCAN_STEP.pack(rows, slots_n, d, n, g, t, 1 if softplus else 0, up, us, dp, ds, zp, zs, bp, bs, cp, cs,
-                                   yp, ys, _par(A, "A", (d, n), f32, dev, False), _par(D, "D", (d,), f32, dev),
-                                   _par(delta_bias, "delta_bias", (d,), f32, dev), state.data_ptr(), state.stride(0), at)
-            _check(_library().sysscan_step(args, s), "sysscan_step")
-        return y
+    if _elsewhere(u, stream):
+        with _there(u, stream, "state_scan_step"):
+            return state_scan_step(u, delta, A, B, C, state, D, z, delta_bias, softplus, slots, out)
+    t, shape = _type(u), u.shape
+    if len(shape) != 2:
+        raise ValueError("u must be (rows, channels)")
+    rows, d = shape
+    n, g = _scan_shapes(u, shape[:1], A, B, C)
+    f32 = torch.float32
+    count = _cache(state, d, n, f32, u)
+    at = _slots(slots, rows, u)
+    if slots is None and count < rows:
+        raise ValueError("state has %d slots for %d rows" % (count, rows))
+    y = torch.empty_like(u, memory_format=_packed_rows) if out is None else out
+    up, _, us = _tok(u, "u", u, shape)
+    dp, _, ds = _tok(delta, "delta", u, shape)
+    zp, _, zs = _tok(z, "z", u, shape) if z is not None else _NONE3
+    bp, _, bs = _bc(B, "B", u, n, g, 1)
+    cp, _, cs = _bc(C, "C", u, n, g, 1)
+    yp, _, ys = _tok(y, "out", u, shape)
+    params = (_par(A, "A", A.shape, f32, u, False), _par(D, "D", (d,), f32, u), _par(delta_bias, "delta_bias", (d,), f32, u))
+    if rows > 0 and d > 0:
+        args = _SCAN_STEP.pack(rows, count, d, n, g, t, 1 if softplus else 0, up, us, dp, ds, zp, zs, bp, bs, cp, cs, yp, ys,
+                               *params, state.data_ptr(), state.stride(0), at)
+        _check(_library().sysscan_step(args, _raw_stream(u.get_device())), "sysscan_step")
+    return y
 
 
 # ---------------------------------------------------------------------------------------------- group norm
@@ -420,17 +425,16 @@ def state_scan_step(u, delta, A, B, C, state, D=None, z=None, delta_bias=None, s
 
 def _norm_view(x, name, like=None):
     """x as (batch, space, channels): the dimensions between the first and the last must have one common stride."""
-    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
+    if like is not None and (x.shape != like.shape or x.dtype is not like.dtype or x.get_device() != like.get_device()):
         raise ValueError("%s must have the shape, type and device of x" % name)
-    if x.dim() < 2:
-        raise ValueError("%s must be (batch, ..., channels)" % name)
     if x.dim() == 3:
         return x
-    b, c = x.shape[0], x.shape[-1]
+    if x.dim() < 2:
+        raise ValueError("%s must be (batch, ..., channels)" % name)
     n = 1
     for v in x.shape[1:-1]:
         n *= v
-    return x.view(b, n, c)
+    return x.view(x.shape[0], n, x.shape[-1])
 
 
 def _norm_head(x, groups, weight, bias, eps, activation):
@@ -441,53 +445,52 @@ def _norm_head(x, groups, weight, bias, eps, activation):
     if groups < 1 or c % groups != 0:
         raise ValueError("%d channels do not divide into %d groups" % (c, groups))
     f32 = torch.float32
-    w = _par(weight, "weight", (c,), f32, x.device)
-    bb = _par(bias, "bias", (c,), f32, x.device)
-    return v, (b, n, c, groups, t, act, float(eps), *_tok(v, "x", v)), w, bb
+    return (v, b, groups, (b, n, c, groups, t, act, float(eps), *_tok(v, "x", v, v.shape)),
+            (_par(weight, "weight", (c,), f32, x), _par(bias, "bias", (c,), f32, x)))
 
 
 def groupnorm(x, groups, weight=None, bias=None, eps=1e-5, activation=None, return_stats=False, out=None, stream=None):
     """Group norm, channels last: x (batch, ..., channels) is normalised over everything between batch and channels and
     over the channels of each group; y = act((x - mean) * rstd * weight + bias).  weight, bias (channels), float32.
     Returns y, or (y, mean, rstd) with return_stats, which groupnorm_backward needs."""
-    with _on(x, stream, "groupnorm") as s:
-        v, head, w, b = _norm_head(x, groups, weight, bias, eps, activation)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        yv = _norm_view(y, "out", x)
-        mean = rstd = None
-        if return_stats:
-            mean = torch.empty((v.shape[0], head[3]), dtype=torch.float32, device=x.device)
-            rstd = torch.empty_like(mean)
-        if x.numel() > 0:
-            lib = _library()
-            body = (*head, *_tok(yv, "out", v), *_NONE3, *_NONE3, w, b, mean.data_ptr() if return_stats else 0,
-                    rstd.data_ptr() if return_stats else 0, 0, 0)
-            args = _NORM.pack(*body, 0, 0)
-            size = _bytes(lib.sysgroupnorm_workspace_bytes(args), "sysgroupnorm")
-            if size:
-                room = _room(size, x.device)
-                args = _NORM.pack(*body, room.data_ptr(), size)
-            _check(lib.sysgroupnorm(args, s), "sysgroupnorm")
-        return (y, mean, rstd) if return_stats else y
+    if _elsewhere(x, stream):
+        with _there(x, stream, "groupnorm"):
+            return groupnorm(x, groups, weight, bias, eps, activation, return_stats, out)
+    v, b, groups, head, params = _norm_head(x, groups, weight, bias, eps, activation)
+    y = torch.empty_like(x, memory_format=_packed_rows) if out is None else out
+    yv = _norm_view(y, "out", x)
+    mean = rstd = None
+    if return_stats:
+        mean, rstd = (torch.empty((b, groups), dtype=torch.float32, device=x.device) for _ in range(2))
+    if x.numel() > 0:
+        lib = _library()
+        body = (*head, *_tok(yv, "out", v, v.shape), *_NONE3, *_NONE3, *params, _ptr(mean), _ptr(rstd), 0, 0)
+        args = _NORM.pack(*body, 0, 0)
+        size = _bytes(lib.sysgroupnorm_workspace_bytes(args), "sysgroupnorm")
+        if size:
+            room = _room(size, x)
+            args = _NORM.pack(*body, room.data_ptr(), size)
+        _check(lib.sysgroupnorm(args, _raw_stream(x.get_device())), "sysgroupnorm")
+    return (y, mean, rstd) if return_stats else y
 
 
 def groupnorm_backward(dy, x, groups, mean, rstd, weight=None, bias=None, activation=None, stream=None):
     """Gradients of groupnorm: (dx, dweight, dbias), the last two None where weight or bias is None."""
-    with _on(x, stream, "groupnorm_backward") as s:
-        v, head, w, b = _norm_head(x, groups, weight, bias, 0.0, activation)
-        dyv = _norm_view(dy, "dy", x)
-        shape = (v.shape[0], head[3])
-        mp = _par(mean, "mean", shape, torch.float32, x.device, False)
-        rp = _par(rstd, "rstd", shape, torch.float32, x.device, False)
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dw = torch.empty_like(weight) if weight is not None else None
-        db = torch.empty_like(bias) if bias is not None else None
-        if x.numel() == 0:
-            return dx, dw.zero_() if dw is not None else None, db.zero_() if db is not None else None
-        lib = _library()
-        body = (*head, *_NONE3, *_tok(dyv, "dy", v), *_tok(_norm_view(dx, "dx"), "dx", v), w, b, mp, rp,
-                dw.data_ptr() if dw is not None else 0, db.data_ptr() if db is not None else 0)
-        size = _bytes(lib.sysgroupnorm_backward_workspace_bytes(_NORM.pack(*body, 0, 0)), "sysgroupnorm_backward")
-        room = _room(size, x.device)
-        _check(lib.sysgroupnorm_backward(_NORM.pack(*body, room.data_ptr() if size else 0, size), s), "sysgroupnorm_backward")
-        return dx, dw, db
+    if _elsewhere(x, stream):
+        with _there(x, stream, "groupnorm_backward"):
+            return groupnorm_backward(dy, x, groups, mean, rstd, weight, bias, activation)
+    v, b, groups, head, params = _norm_head(x, groups, weight, bias, 0.0, activation)
+    dyv = _norm_view(dy, "dy", x)
+    stats = (_par(mean, "mean", (b, groups), torch.float32, x, False), _par(rstd, "rstd", (b, groups), torch.float32, x, False))
+    dx = torch.empty_like(x, memory_format=_packed_rows)
+    dw = torch.empty_like(weight) if weight is not None else None
+    db = torch.empty_like(bias) if bias is not None else None
+    if x.numel() == 0:
+        return dx, dw.zero_() if dw is not None else None, db.zero_() if db is not None else None
+    lib = _library()
+    body = (*head, *_NONE3, *_tok(dyv, "dy", v, v.shape), *_tok(_norm_view(dx, "dx"), "dx", v, v.shape), *params, *stats,
+            _ptr(dw), _ptr(db))
+    size = _bytes(lib.sysgroupnorm_backward_workspace_bytes(_NORM.pack(*body, 0, 0)), "sysgroupnorm_backward")
+    room = _room(size, x)
+    _check(lib.sysgroupnorm_backward(_NORM.pack(*body, _ptr(room), size), _raw_stream(x.get_device())), "sysgroupnorm_backward")
+    return dx, dw, db
