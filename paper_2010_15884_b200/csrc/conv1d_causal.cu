@@ -13,6 +13,8 @@ namespace {
 
 constexpr int kThreads = 128;
 
+template <int N> struct Count { static constexpr int value = N; };
+
 template <typename T>
 __device__ __forceinline__ float load_param(const void *p, long long i, bool f32)
 {
@@ -33,38 +35,50 @@ struct CausalArgs {
     bool weight_f32, silu;
 };
 
+// Filter and bias of V channels from c on: w[k], the channels packed in pairs.  The V x K numbers are contiguous.
+template <typename T, int V, int K>
+__device__ __forceinline__ void load_filter(const CausalArgs &a, int c, Vec<V> (&w)[K], Vec<V> &bias)
+{
+    float f[V * K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {                                   // V numbers at a time
+        const Vec<V> v = load_params<T, V>(a.weight, static_cast<long long>(c) * K + i * V, a.weight_f32, V > 1, 0.0f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[i * V + j] = v.get(j);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        w[k] = each<V>([&](int i) { return pair(f[2 * i * K + k], 2 * i + 1 < V ? f[(2 * i + 1) * K % (V * K) + k] : 0.0f); });
+    bias = load_params<T, V>(a.bias, c, a.weight_f32, V > 1, 0.0f);
+}
+
 // Row p of a sequence's line before its first token (p in [-(K-1), 0)), from its state; zeros without one.
 template <typename T, int V, int K>
-__device__ __forceinline__ void load_before(const CausalArgs &a, const void *state, int r, long long p, int c, float (&f)[V])
+__device__ __forceinline__ Vec<V> load_before(const CausalArgs &a, int r, long long p, int c)
 {
-    if (state == nullptr) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = 0.0f;
-        return;
-    }
+    if (a.state == nullptr) return splat<V>(0.0f);
     const long long row = p < -(K - 1) ? 0 : K - 1 + p;            // a wrong offset cannot lead outside the state
-    unpack(load_pack<T, V>(static_cast<const T *>(state) + (static_cast<long long>(r) * (K - 1) + row) * a.channels + c), f);
+    return widen(load_pack<T, V>(static_cast<const T *>(a.state) + (static_cast<long long>(r) * (K - 1) + row) * a.channels + c));
 }
 
 // The K-1 inputs before flat token t of sequence r (first token `first`), oldest first.
 template <typename T, int V, int K>
-__device__ __forceinline__ void load_window(const CausalArgs &a, int r, long long first, long long t, int c, float (&win)[K][V])
+__device__ __forceinline__ void load_window(const CausalArgs &a, int r, long long first, long long t, int c, Vec<V> *win)
 {
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
         const long long q = t - (K - 1) + j;
-        if (q >= first) unpack(load_pack<T, V>(token_row<T>(a.x, a.map, r, q) + c), win[j]);
-        else load_before<T, V, K>(a, a.state, r, q - first, c, win[j]);
+        win[j] = q >= first ? widen(load_pack<T, V>(token_row<T>(a.x, a.map, r, q) + c)) : load_before<T, V, K>(a, r, q - first, c);
     }
 }
 
 template <typename T, int V, int K>
-__device__ __forceinline__ void store_state(const CausalArgs &a, int r, int c, const float (&win)[K][V])
+__device__ __forceinline__ void store_state(const CausalArgs &a, int r, int c, const Vec<V> *win)
 {
     if (a.final_state == nullptr) return;
 #pragma unroll
     for (int j = 0; j < K - 1; ++j)
-        store_pack(static_cast<T *>(a.final_state) + (static_cast<long long>(r) * (K - 1) + j) * a.channels + c, pack<T, V>(win[j]));
+        store_pack(static_cast<T *>(a.final_state) + (static_cast<long long>(r) * (K - 1) + j) * a.channels + c, narrow<T, V>(win[j]));
 }
 
 // The final state of every empty sequence from r on whose place is flat token t; returns the first sequence that is not.
@@ -72,7 +86,7 @@ template <typename T, int V, int K>
 __device__ __forceinline__ int pass_empty(const CausalArgs &a, int r, long long t, int c)
 {
     while (r < a.map.sequences && a.map.end(r) <= t) {
-        float win[K][V];
+        Vec<V> win[K];
         load_window<T, V, K>(a, r, t, t, c, win);
         store_state<T, V, K>(a, r, c, win);
         ++r;
@@ -80,11 +94,13 @@ __device__ __forceinline__ int pass_empty(const CausalArgs &a, int r, long long 
     return r;
 }
 
+constexpr int kAhead = 4;                // tokens per step of a thread; the next step's loads are in flight meanwhile
+
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
 {
     dependent_launch_enter();
-    constexpr int U = 8;                                            // tokens in flight per thread
+    constexpr int U = kAhead;
     const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     const long long run = id / a.groups;
     if (run >= a.runs) return;
@@ -92,47 +108,56 @@ __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
     long long t = run * a.run;
     const long long stop = min(t + a.run, a.map.total);
 
-    float w[K][V], bias[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) w[k][i] = load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32);
-        bias[i] = a.bias ? load_param<T>(a.bias, c + i, a.weight_f32) : 0.0f;
-    }
+    Vec<V> w[K], bias;
+    load_filter<T, V, K>(a, c, w, bias);
     int r = t == 0 ? pass_empty<T, V, K>(a, 0, 0, c) : a.map.find(t);
     while (t < stop && r < a.map.sequences) {
         const long long first = a.map.first(r), end = a.map.end(r);
-        const long long last = min(end, stop);
-        float win[K][V];                                            // the K-1 inputs before t; win[K-1]: the input of t
-        load_window<T, V, K>(a, r, first, t, c, win);
+        int left = static_cast<int>(min(end, stop) - t);            // (negative: descending offsets)
+        Vec<V> line[K - 1 + U];                                     // the K-1 inputs before t, then U of them from t on
+        load_window<T, V, K>(a, r, first, t, c, line);
         const T *src = token_row<T>(a.x, a.map, r, t) + c;
         T *dst = token_row<T>(a.y, a.map, r, t) + c;
-        auto step = [&](const Pack<T, V> &raw, T *to) {
-            unpack(raw, win[K - 1]);
-            float out[V];
+        const long long xs = a.x.tstride, ys = a.y.tstride;
+        if (left > 0) t += left;
+        auto outputs = [&](auto count) {
+            constexpr int N = decltype(count)::value;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float v = bias[i];
+            for (int u = 0; u < N; ++u) {
+                Vec<V> v = bias;
 #pragma unroll
-                for (int k = 0; k < K; ++k) v = fmaf(w[k][i], win[k][i], v);
-                out[i] = a.silu ? silu(v) : v;
+                for (int k = 0; k < K; ++k) v = fma2(w[k], line[u + k], v);
+                if (a.silu) v = silu2(v);
+                store_pack(dst + u * ys, narrow<T, V>(v));
             }
-            store_pack(to, pack<T, V>(out));
 #pragma unroll
-            for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
+            for (int k = 0; k < K - 1; ++k) line[k] = line[N + k];
+            dst += N * ys;
+            left -= N;
         };
-        for (; t + U <= last; t += U, src += U * a.x.tstride, dst += U * a.y.tstride) {
-            Pack<T, V> raw[U];
+        Pack<T, V> raw[U];
+        if (left >= U) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = load_pack<T, V>(src + u * a.x.tstride);
-#pragma unroll
-            for (int u = 0; u < U; ++u) step(raw[u], dst + u * a.y.tstride);
+            for (int u = 0; u < U; ++u) raw[u] = load_pack<T, V>(src + u * xs);
+            src += U * xs;
         }
-        for (; t < last; ++t, src += a.x.tstride, dst += a.y.tstride) step(load_pack<T, V>(src), dst);
+        while (left >= U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) line[K - 1 + u] = widen(raw[u]);
+            if (left >= 2 * U) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u] = load_pack<T, V>(src + u * xs);
+                src += U * xs;
+            }
+            outputs(Count<U>{});
+        }
+        while (left > 0) {
+            line[K - 1] = widen(load_pack<T, V>(src));
+            src += xs;
+            outputs(Count<1>{});
+        }
         if (t >= end) {                                             // (t > end: descending offsets; never loop on them)
-            store_state<T, V, K>(a, r, c, win);
+            store_state<T, V, K>(a, r, c, line);
             r = pass_empty<T, V, K>(a, r + 1, t, c);
         }
     }
@@ -142,56 +167,43 @@ __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
 // pass, and the last K of them give dx[t-(K-1)] = sum_k w[k] dpre[t-k], so both windows live in registers and a token's
 // x and dy are read once (the K-1 tokens behind a run a second time).  The sums for dweight and dbias stay in registers
 // over the run, are added over the block's runs in shared memory and leave as one partial row per block row; a second
-// kernel adds the rows in a fixed order.
+// kernel adds the rows in a fixed order.  Steps whose tokens and outputs all lie inside the run and the sequence go
+// kAhead at a time without a test; the others one by one.
 constexpr int kBackRows = 4;             // runs per block, 32 threads (groups of V channels) each
 
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalArgs a)
 {
     dependent_launch_enter();
+    constexpr int U = kAhead;
     const int group = blockIdx.x * 32 + threadIdx.x;
     const long long run = static_cast<long long>(blockIdx.y) * kBackRows + threadIdx.y;
     const bool live = group < a.groups && run < a.runs;
     const int c = live ? group * V : 0;
-    float w[K][V], bias[V], dw[K][V], db[V];
+    Vec<V> dw[K], db = splat<V>(0.0f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            w[k][i] = load_param<T>(a.weight, static_cast<long long>(c + i) * K + k, a.weight_f32);
-            dw[k][i] = 0.0f;
-        }
-        bias[i] = a.bias ? load_param<T>(a.bias, c + i, a.weight_f32) : 0.0f;
-        db[i] = 0.0f;
-    }
+    for (int k = 0; k < K; ++k) dw[k] = splat<V>(0.0f);
     if (live) {
+        Vec<V> w[K], bias;
+        load_filter<T, V, K>(a, c, w, bias);
         const long long start = run * a.run, stop = min(start + a.run, a.map.total);
         long long t = start;
         int r = t == 0 ? 0 : a.map.find(t);
-        // dL/dline row s of sequence r (s < 0: state): `sum` and what comes through the final state
-        auto emit = [&](int rr, long long first, long long end, long long s, float (&f)[V]) {
-            if (a.dfinal != nullptr && s >= end - (K - 1)) {
-                float g[V];
-                unpack(load_pack<T, V>(static_cast<const T *>(a.dfinal) +
-                                       (static_cast<long long>(rr) * (K - 1) + (s - end + K - 1)) * a.channels + c), g);
-#pragma unroll
-                for (int i = 0; i < V; ++i) f[i] += g[i];
-            }
+        // dL/dline row s of sequence r (s before `first`: its state): f, and what comes through the final state
+        auto emit = [&](int rr, long long first, long long end, long long s, Vec<V> f) {
+            if (a.dfinal != nullptr && s >= end - (K - 1))
+                f = add2(f, widen(load_pack<T, V>(static_cast<const T *>(a.dfinal) +
+                                                  (static_cast<long long>(rr) * (K - 1) + (s - end + K - 1)) * a.channels + c)));
             if (s >= first) {
-                if (a.dx.ptr != nullptr) store_pack(token_row<T>(a.dx, a.map, rr, s) + c, pack<T, V>(f));
+                if (a.dx.ptr != nullptr) store_pack(token_row<T>(a.dx, a.map, rr, s) + c, narrow<T, V>(f));
             } else if (a.dstate != nullptr) {
                 store_pack(static_cast<T *>(a.dstate) + (static_cast<long long>(rr) * (K - 1) + (s - first + K - 1)) * a.channels + c,
-                           pack<T, V>(f));
+                           narrow<T, V>(f));
             }
         };
         auto pass_empty_back = [&](int rr, long long at) {
             while (rr < a.map.sequences && a.map.end(rr) <= at) {
-                for (int j = 0; j < K - 1; ++j) {
-                    float f[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) f[i] = 0.0f;
-                    emit(rr, at, at, at - (K - 1) + j, f);
-                }
+                for (int j = 0; j < K - 1; ++j) emit(rr, at, at, at - (K - 1) + j, splat<V>(0.0f));
                 ++rr;
             }
             return rr;
@@ -202,74 +214,92 @@ __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalA
             const long long mine = min(end, stop);                   // tokens whose sums and dx are this run's
             const long long last = min(end, mine + K - 1);           // tokens whose dpre they need
             const long long from = t > first ? t : first - (K - 1);  // line rows that are this run's
-            float win[K][V], g[K][V];                                // g[k]: dpre of token t-k
-            load_window<T, V, K>(a, r, first, t, c, win);
+            const long long flush = end <= mine + K - 1 ? end + K - 1 : last;   // past the end dpre is zero
+            const long long xs = a.x.tstride, ys = a.y.tstride, os = a.dx.tstride;
+            Vec<V> line[K - 1 + U], g[K - 1 + U];                    // g[j]: dpre of token t - (K-1) + j
+            load_window<T, V, K>(a, r, first, t, c, line);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) g[k][i] = 0.0f;
+            for (int k = 0; k < K - 1; ++k) g[k] = splat<V>(0.0f);
             const T *src = token_row<T>(a.x, a.map, r, t) + c;
             const T *dsrc = token_row<T>(a.y, a.map, r, t) + c;
-            constexpr int U = 2;
-            const long long flush = end <= mine + K - 1 ? end + K - 1 : last;   // past the end dpre is zero
-            while (t < flush) {
-                const int n = static_cast<int>(min(flush - t, static_cast<long long>(U)));
+            auto slope_of = [&](int u, const Vec<V> &dy) {           // dpre of the token whose window starts at line[u]
+                if (!a.silu) return dy;
+                Vec<V> v = bias;
+#pragma unroll
+                for (int k = 0; k < K; ++k) v = fma2(w[k], line[u + k], v);
+                return mul2(dy, silu_slope2(v));
+            };
+            auto gather = [&](int u) {                               // dL/dline of the oldest token in g[u ..]
+                Vec<V> f = mul2(w[0], g[u + K - 1]);
+#pragma unroll
+                for (int k = 1; k < K; ++k) f = fma2(w[k], g[u + K - 1 - k], f);
+                return f;
+            };
+            auto accumulate = [&](int u) {
+                db = add2(db, g[u + K - 1]);
+#pragma unroll
+                for (int k = 0; k < K; ++k) dw[k] = fma2(g[u + K - 1], line[u + k], dw[k]);
+            };
+            auto one = [&]() {
+                if (t < last) {
+                    line[K - 1] = widen(load_pack<T, V>(src));
+                    g[K - 1] = slope_of(0, widen(load_pack<T, V>(dsrc)));
+                    if (t < mine) accumulate(0);
+#pragma unroll
+                    for (int k = 0; k < K - 1; ++k) line[k] = line[k + 1];
+                } else {
+                    g[K - 1] = splat<V>(0.0f);
+                }
+                const long long s = t - (K - 1);
+                if (s >= from && s < mine) emit(r, first, end, s, gather(0));
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k) g[k] = g[k + 1];
+                ++t;
+                src += xs;
+                dsrc += ys;
+            };
+            // rows before the first of this run's tokens
+            for (int k = 0; k < K - 1 && t < flush; ++k) one();
+            T *out = a.dx.ptr != nullptr ? token_row<T>(a.dx, a.map, r, t - (K - 1)) + c : nullptr;
+            if (t + U <= mine) {
                 Pack<T, V> xr[U], yr[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (t + u < last) {
-                        xr[u] = load_pack<T, V>(src + u * a.x.tstride);
-                        yr[u] = load_pack<T, V>(dsrc + u * a.y.tstride);
-                    }
-#pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (u < n) {
-                        if (t + u < last) {
-                            float dy[V];
-                            unpack(xr[u], win[K - 1]);
-                            unpack(yr[u], dy);
-#pragma unroll
-                            for (int i = 0; i < V; ++i) {
-                                float v = bias[i];
-#pragma unroll
-                                for (int k = 0; k < K; ++k) v = fmaf(w[k][i], win[k][i], v);
-                                const float d = a.silu ? dy[i] * silu_slope(v, sigmoid(v)) : dy[i];
-                                g[0][i] = d;
-                                if (t + u < mine) {
-                                    db[i] += d;
-#pragma unroll
-                                    for (int k = 0; k < K; ++k) dw[k][i] = fmaf(d, win[k][i], dw[k][i]);
-                                }
-                            }
-#pragma unroll
-                            for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                                for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
-                        }
-                        const long long s = t + u - (K - 1);
-                        if (s >= from && s < mine) {
-                            float f[V];
-#pragma unroll
-                            for (int i = 0; i < V; ++i) {
-                                f[i] = 0.0f;
-#pragma unroll
-                                for (int k = 0; k < K; ++k) f[i] = fmaf(w[k][i], g[k][i], f[i]);
-                            }
-                            emit(r, first, end, s, f);
-                        }
-#pragma unroll
-                        for (int k = K - 1; k > 0; --k)
-#pragma unroll
-                            for (int i = 0; i < V; ++i) g[k][i] = g[k - 1][i];
-                    }
+                    xr[u] = load_pack<T, V>(src + u * xs);
+                    yr[u] = load_pack<T, V>(dsrc + u * ys);
                 }
-                t += n;
-                src += n * a.x.tstride;
-                dsrc += n * a.y.tstride;
+                while (t + U <= mine) {
+                    Vec<V> dy[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        line[K - 1 + u] = widen(xr[u]);
+                        dy[u] = widen(yr[u]);
+                    }
+                    t += U;
+                    src += U * xs;
+                    dsrc += U * ys;
+                    if (t + U <= mine) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            xr[u] = load_pack<T, V>(src + u * xs);
+                            yr[u] = load_pack<T, V>(dsrc + u * ys);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        g[K - 1 + u] = slope_of(u, dy[u]);
+                        accumulate(u);
+                        if (out != nullptr) store_pack(out + u * os, narrow<T, V>(gather(u)));
+                    }
+#pragma unroll
+                    for (int k = 0; k < K - 1; ++k) {
+                        line[k] = line[U + k];
+                        g[k] = g[U + k];
+                    }
+                    if (out != nullptr) out += U * os;
+                }
             }
+            while (t < flush) one();
             t = max(start_t, mine);                                  // (mine < start_t: descending offsets)
             if (t >= end) r = pass_empty_back(r + 1, t);
         }
@@ -279,8 +309,8 @@ __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalA
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) sums[threadIdx.y][k * V + i][threadIdx.x] = dw[k][i];
-        sums[threadIdx.y][K * V + i][threadIdx.x] = db[i];
+        for (int k = 0; k < K; ++k) sums[threadIdx.y][k * V + i][threadIdx.x] = dw[k].get(i);
+        sums[threadIdx.y][K * V + i][threadIdx.x] = db.get(i);
     }
     __syncthreads();
     for (int e = threadIdx.y * 32 + threadIdx.x; e < (K + 1) * V * 32; e += 32 * kBackRows) {
@@ -414,7 +444,8 @@ int run_length(long long total, long long groups, long long threads, int most)
 
 bool state_aligned(const sysconv_causal_args &a, size_t esz, size_t bytes)
 {
-    return a.channels * esz % bytes == 0 && ptr_aligned(a.state, bytes) && ptr_aligned(a.final_state, bytes) &&
+    const size_t wide = a.weight_type == SYSCONV_T_F32 ? 16 : 8;     // four parameters
+    return ptr_aligned(a.weight, wide) && ptr_aligned(a.bias, wide) && a.channels * esz % bytes == 0 && ptr_aligned(a.state, bytes) && ptr_aligned(a.final_state, bytes) &&
            ptr_aligned(a.dfinal, bytes) && ptr_aligned(a.dstate, bytes);
 }
 
@@ -452,7 +483,7 @@ cudaError_t launch_causal(const sysconv_causal_args &a, cudaStream_t s, int *lau
                               state_aligned(a, sizeof(T), bytes);
             CausalArgs k = base_args(a);
             k.groups = wide ? k.channels / V : k.channels;
-            k.run = run_length(k.map.total, k.groups, 148LL * 1024, 16);
+            k.run = run_length(k.map.total, k.groups, 148LL * 1024, 32);
             k.runs = k.map.total > 0 ? (k.map.total + k.run - 1) / k.run : 1;
             const long long blocks = (k.runs * k.groups + kThreads - 1) / kThreads;
             if (blocks > 0x7fffffffLL) return kNoInstantiation;

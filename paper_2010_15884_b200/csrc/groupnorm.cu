@@ -30,7 +30,7 @@ struct NormArgs {
     int channels, groups, cg;
     float eps;
     bool silu;
-    int tile_groups;             // slab form: groups per block
+    int tile;                    // slab form: channels per block
     int rows_per_slab, slabs;
     int entry_step;              // warp form: batch entries handled side by side
 };
@@ -60,59 +60,68 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
     const int lane = threadIdx.x & 31;
     const long long w = static_cast<long long>(blockIdx.x) * (kNormThreads / 32) + (threadIdx.x >> 5);
     const int g = static_cast<int>(w % a.groups);
-    long long b = w / a.groups;
-    const long long row = b;
+    const long long row = w / a.groups;
     if (row >= a.entry_step) return;
     const int per_row = a.cg / V;
     const int count = static_cast<int>(a.space) * per_row;               // vectors of the group
     const float inv = 1.0f / static_cast<float>(static_cast<long long>(count) * V);
-    int at_s[R], at_c[R];
-    float wv[R][V], bv[R][V];
-    float db[BACK ? R : 1][V], dw[BACK ? R : 1][V];
+    // offsets of this lane's vectors within a batch entry; those that do not exist repeat the first one and do not count
+    long long at_x[R], at_y[R], at_d[BACK ? R : 1];
+    int at_c[R];
+    bool ok[R];
+    Vec<V> wv[R], bv[R], db[BACK ? R : 1], dw[BACK ? R : 1];
+    const Tokens &out_t = BACK ? a.dx : a.y;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        const int q = lane + 32 * i;
-        at_s[i] = q / per_row;
-        at_c[i] = g * a.cg + (q - at_s[i] * per_row) * V;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            wv[i][j] = q < count && a.w ? a.w[at_c[i] + j] : 1.0f;
-            bv[i][j] = q < count && a.b ? a.b[at_c[i] + j] : 0.0f;
-            if (BACK) db[i][j] = dw[i][j] = 0.0f;
-        }
+        ok[i] = lane + 32 * i < count;
+        const int q = ok[i] ? lane + 32 * i : 0, s = q / per_row;
+        at_c[i] = g * a.cg + (q - s * per_row) * V;
+        at_x[i] = s * a.x.tstride + at_c[i];
+        at_y[i] = s * out_t.tstride + at_c[i];
+        if (BACK) at_d[i] = s * a.dy.tstride + at_c[i];
+        wv[i] = load_params<float, V>(a.w, at_c[i], true, false, 1.0f);
+        bv[i] = load_params<float, V>(a.b, at_c[i], true, false, 0.0f);
+        if (BACK) db[i] = dw[i] = splat<V>(0.0f);
     }
     Pack<T, V> raw[R], rdy[BACK ? R : 1];
-    auto fetch = [&](long long e) {
+    const T *px = static_cast<const T *>(a.x.ptr) + row * a.x.bstride;
+    const T *pd = BACK ? static_cast<const T *>(a.dy.ptr) + row * a.dy.bstride : nullptr;
+    T *po = static_cast<T *>(out_t.ptr) + row * out_t.bstride;
+    auto fetch = [&]() {
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (lane + 32 * i < count) {
-                raw[i] = load_pack<T, V>(norm_at<T>(a.x, e, at_s[i], at_c[i]));
-                if (BACK) rdy[i] = load_pack<T, V>(norm_at<T>(a.dy, e, at_s[i], at_c[i]));
-            }
+        for (int i = 0; i < R; ++i) {
+            raw[i] = load_pack<T, V>(px + at_x[i]);
+            if (BACK) rdy[i] = load_pack<T, V>(pd + at_d[i]);
+        }
+        px += a.entry_step * a.x.bstride;
+        if (BACK) pd += a.entry_step * a.dy.bstride;
     };
-    if (b < a.batch) fetch(b);
-    for (; b < a.batch; b += a.entry_step) {
-        float x[R][V], e[BACK ? R : 1][V];
+    if (row < a.batch) fetch();
+    for (long long b = row; b < a.batch; b += a.entry_step) {
+        Vec<V> x[R], e[BACK ? R : 1];
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                x[i][j] = raw[i].get(j);
-                if (BACK) e[i][j] = rdy[i].get(j);
-            }
-        const float shift = __shfl_sync(kFullMask, x[0][0], 0);
-        if (b + a.entry_step < a.batch) fetch(b + a.entry_step);
+        for (int i = 0; i < R; ++i) {
+            x[i] = widen(raw[i]);
+            if (BACK) e[i] = widen(rdy[i]);
+        }
+        if (b + a.entry_step < a.batch) fetch();
         if (!BACK) {
+            const float shift = __shfl_sync(kFullMask, x[0].get(0), 0);
+            Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const Vec<V> v = add2(x[i], splat<V>(ok[i] ? -shift : -x[i].get(0)));
+                if (ok[i]) {
+                    s1 = add2(s1, v);
+                    s2 = fma2(v, v, s2);
+                }
+            }
             float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (lane + 32 * i < count)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float v = x[i][j] - shift;
-                        s.x += v;
-                        s.y = fmaf(v, v, s.y);
-                    }
+            for (int j = 0; j < V; ++j) {
+                s.x += s1.get(j);
+                s.y += s2.get(j);
+            }
             s = warp_sum(s);
             const float off = s.x * inv, mean = shift + off;
             const float rstd = rsqrtf(fmaxf(fmaf(-off, off, s.y * inv), 0.0f) + a.eps);
@@ -121,69 +130,61 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
                 if (a.rstd) a.rstd[b * a.groups + g] = rstd;
             }
 #pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (lane + 32 * i < count) {
-                    float out[V];
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float v = fmaf((x[i][j] - mean) * rstd, wv[i][j], bv[i][j]);
-                        out[j] = a.silu ? silu(v) : v;
-                    }
-                    store_pack(norm_at<T>(a.y, b, at_s[i], at_c[i]), pack<T, V>(out));
-                }
+            for (int i = 0; i < R; ++i) {
+                Vec<V> v = fma2(add2(x[i], splat<V>(-mean)), mul2(wv[i], splat<V>(rstd)), bv[i]);
+                if (a.silu) v = silu2(v);
+                if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(v));
+            }
         } else {
             const float mean = a.mean[b * a.groups + g], rstd = a.rstd[b * a.groups + g];
+            Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                x[i] = mul2(add2(x[i], splat<V>(-mean)), splat<V>(rstd));
+                if (a.silu) e[i] = mul2(e[i], silu_slope2(fma2(x[i], wv[i], bv[i])));
+                if (ok[i]) {
+                    db[i] = add2(db[i], e[i]);
+                    dw[i] = fma2(e[i], x[i], dw[i]);
+                    e[i] = mul2(e[i], wv[i]);
+                    s1 = add2(s1, e[i]);
+                    s2 = fma2(e[i], x[i], s2);
+                }
+            }
             float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (lane + 32 * i < count)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float xh = (x[i][j] - mean) * rstd;
-                        if (a.silu) {
-                            const float v = fmaf(xh, wv[i][j], bv[i][j]);
-                            e[i][j] *= silu_slope(v, sigmoid(v));
-                        }
-                        db[i][j] += e[i][j];
-                        dw[i][j] = fmaf(e[i][j], xh, dw[i][j]);
-                        const float p = e[i][j] * wv[i][j];
-                        s.x += p;
-                        s.y = fmaf(p, xh, s.y);
-                        x[i][j] = xh;
-                    }
+            for (int j = 0; j < V; ++j) {
+                s.x += s1.get(j);
+                s.y += s2.get(j);
+            }
             s = warp_sum(s);
-            s.x *= inv;
-            s.y *= inv;
+            const Vec<V> m1 = splat<V>(-s.x * inv), m2 = splat<V>(-s.y * inv);
 #pragma unroll
             for (int i = 0; i < R; ++i)
-                if (lane + 32 * i < count) {
-                    float out[V];
-#pragma unroll
-                    for (int j = 0; j < V; ++j) out[j] = rstd * (fmaf(e[i][j], wv[i][j], -s.x) - x[i][j] * s.y);
-                    store_pack(norm_at<T>(a.dx, b, at_s[i], at_c[i]), pack<T, V>(out));
-                }
+                if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(mul2(splat<V>(rstd), add2(fma2(x[i], m2, m1), e[i]))));
         }
+        po += a.entry_step * out_t.bstride;
     }
     if (BACK && a.pq != nullptr) {                                       // space is 1 here: a channel belongs to one lane
 #pragma unroll
         for (int i = 0; i < R; ++i)
-            if (lane + 32 * i < count)
+            if (ok[i])
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    a.pq[row * 2 * a.channels + at_c[i] + j] = db[i][j];
-                    a.pq[(row * 2 + 1) * a.channels + at_c[i] + j] = dw[i][j];
+                    a.pq[row * 2 * a.channels + at_c[i] + j] = db[i].get(j);
+                    a.pq[(row * 2 + 1) * a.channels + at_c[i] + j] = dw[i].get(j);
                 }
     }
 }
 
 // ---- slabs -----------------------------------------------------------------------------------------------------------
-// A block takes a slab of rows and `tile_groups` groups.  If a row of the tile has at most 256 vectors, a thread keeps one
-// channel vector and walks down the rows; else (one wide group) the threads share the rows' vectors.
+// A block takes a slab of rows and a tile of `tile` channels (all of them, or some whole groups).  If a row of the tile has
+// at most 256 vectors, a thread keeps one channel vector and walks down the rows; else (one wide group) it does so for every
+// 256th of them.  Sums are kept per channel, so a vector may lie across groups.
 
 struct SlabPlace {
     long long b, row0, row1;
-    int g0, ng, per_row;         // groups of the tile, vectors per row
-    int cv, r0, step;            // own vector (walking form), first row, rows per step
+    int c0, channels, per_row;   // first channel, channels and vectors per row of the tile
+    int cv, r0, step;            // own vector, first row, rows per step
     bool walk, live;
 };
 
@@ -194,9 +195,9 @@ __device__ __forceinline__ SlabPlace slab_place(const NormArgs &a, int slab)
     p.b = blockIdx.z;
     p.row0 = static_cast<long long>(slab) * a.rows_per_slab;
     p.row1 = min(p.row0 + a.rows_per_slab, a.space);
-    p.g0 = blockIdx.y * a.tile_groups;
-    p.ng = min(a.tile_groups, a.groups - p.g0);
-    p.per_row = p.ng * (a.cg / V);
+    p.c0 = blockIdx.y * a.tile;
+    p.channels = min(a.tile, a.channels - p.c0);
+    p.per_row = p.channels / V;
     p.walk = p.per_row <= kNormThreads;
     p.step = p.walk ? kNormThreads / p.per_row : 1;
     p.r0 = p.walk ? threadIdx.x / p.per_row : 0;
@@ -205,82 +206,150 @@ __device__ __forceinline__ SlabPlace slab_place(const NormArgs &a, int slab)
     return p;
 }
 
+// f(packs of rows u = 0 .. n-1) over this thread's rows, UN at a time with the next ones' loads in flight, then one by one
+template <typename T, int V, int UN, bool TWO, typename F>
+__device__ __forceinline__ void walk_rows(const SlabPlace &p, const T *x, long long sx, const T *y, long long sy, F f)
+{
+    long long left = p.row1 - (p.row0 + p.r0);
+    int n = left <= 0 ? 0 : static_cast<int>((left + p.step - 1) / p.step);
+    Pack<T, V> a[UN], b[TWO ? UN : 1];
+    auto load = [&](int count) {
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+            if (u < count) {
+                a[u] = load_pack<T, V>(x + u * sx);
+                if (TWO) b[u] = load_pack<T, V>(y + u * sy);
+            }
+        x += UN * sx;
+        if (TWO) y += UN * sy;
+    };
+    if (n >= UN) load(UN);
+    while (n >= UN) {
+        Vec<V> va[UN], vb[TWO ? UN : 1];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            va[u] = widen(a[u]);
+            if (TWO) vb[u] = widen(b[u]);
+        }
+        n -= UN;
+        if (n >= UN) load(UN);
+#pragma unroll
+        for (int u = 0; u < UN; ++u) f(va[u], vb[TWO ? u : 0]);
+    }
+    while (n > 0) {
+        const Vec<V> va = widen(load_pack<T, V>(x));
+        Vec<V> vb;
+        if (TWO) vb = widen(load_pack<T, V>(y));
+        f(va, vb);
+        x += sx;
+        if (TWO) y += sy;
+        --n;
+    }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ Vec<V> per_channel(int c, int cg, const float *from)      // from[group of channel]
+{
+    float f[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = from[(c + j) / cg];
+    return each<V>([&](int i) { return pair(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.0f); });
+}
+
+// Per channel sums of a block's threads: s1 and s2 over the threads that share a vector, into chan[2][channels of the tile].
+template <int V>
+__device__ __forceinline__ void add_rows(const SlabPlace &p, const Vec<V> &s1, const Vec<V> &s2, float (*sums)[kNormThreads], float *chan)
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        sums[j][threadIdx.x] = s1.get(j);
+        sums[V + j][threadIdx.x] = s2.get(j);
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < 2 * p.channels; q += kNormThreads) {
+        const int which = q / p.channels, ch = q - which * p.channels;
+        float v = 0.0f;
+        for (int r = 0; r < p.step; ++r) v += sums[which * V + ch % V][r * p.per_row + ch / V];
+        chan[q] = v;
+    }
+    __syncthreads();
+}
+
 template <typename T, int V>
 __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs a)
 {
     dependent_launch_enter();
     const SlabPlace p = slab_place<V>(a, blockIdx.x);
-    __shared__ float2 sums[kNormThreads];
-    float2 s = make_float2(0.0f, 0.0f);
-    if (p.live) {
-        constexpr int UN = 4;
+    __shared__ float sums[2 * V][kNormThreads], chan[2 * V * kNormThreads];
+    Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
+    if (p.live)
         for (int cv = p.cv; cv < p.per_row; cv += kNormThreads) {        // once in the walking form
-            const int c = p.g0 * a.cg + cv * V;
-            const float shift = to_f32(*norm_at<T>(a.x, p.b, 0, c / a.cg * a.cg));
-            const T *src = norm_at<T>(a.x, p.b, p.row0 + p.r0, c);
-            const long long step = p.step * a.x.tstride;
-            long long row = p.row0 + p.r0;
-            for (; row + (UN - 1) * p.step < p.row1; row += UN * p.step, src += UN * step) {
-                Pack<T, V> raw[UN];
+            const int c = p.c0 + cv * V;
+            float k[V];
 #pragma unroll
-                for (int u = 0; u < UN; ++u) raw[u] = load_pack<T, V>(src + u * step);
-#pragma unroll
-                for (int u = 0; u < UN; ++u)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float v = raw[u].get(j) - shift;
-                        s.x += v;
-                        s.y = fmaf(v, v, s.y);
-                    }
-            }
-            for (; row < p.row1; row += p.step, src += step) {
-                const Pack<T, V> raw = load_pack<T, V>(src);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float v = raw.get(j) - shift;
-                    s.x += v;
-                    s.y = fmaf(v, v, s.y);
-                }
-            }
+            for (int j = 0; j < V; ++j) k[j] = -to_f32(*norm_at<T>(a.x, p.b, 0, (c + j) / a.cg * a.cg));
+            const Vec<V> shift = each<V>([&](int i) { return pair(k[2 * i], 2 * i + 1 < V ? k[2 * i + 1] : 0.0f); });
+            walk_rows<T, V, 4, false>(p, norm_at<T>(a.x, p.b, p.row0 + p.r0, c), p.step * a.x.tstride, static_cast<const T *>(nullptr), 0,
+                                      [&](const Vec<V> &x, const Vec<V> &) {
+                                          const Vec<V> v = add2(x, shift);
+                                          s1 = add2(s1, v);
+                                          s2 = fma2(v, v, s2);
+                                      });
         }
+    // groups of the tile, one warp each: their channels' sums, or (one wide group) every thread's
+    int per = a.cg, groups = p.channels / a.cg;
+    if (p.walk) {
+        add_rows<V>(p, s1, s2, sums, chan);
+    } else {
+        float t1 = 0.0f, t2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            t1 += s1.get(j);
+            t2 += s2.get(j);
+        }
+        chan[threadIdx.x] = t1;
+        chan[kNormThreads + threadIdx.x] = t2;
+        per = kNormThreads;
+        groups = 1;
+        __syncthreads();
     }
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    // one warp per group: its entries of the rows-by-vectors grid of partial sums
-    const int lane = threadIdx.x & 31, vg = a.cg / V;
-    for (int g = threadIdx.x >> 5; g < p.ng; g += kNormThreads / 32) {
+    const int lane = threadIdx.x & 31;
+    for (int g = threadIdx.x >> 5; g < groups; g += kNormThreads / 32) {
         float2 t = make_float2(0.0f, 0.0f);
-        const int n = p.walk ? p.step * vg : kNormThreads;
-        for (int i = lane; i < n; i += 32) {
-            const int at = p.walk ? i / vg * p.per_row + g * vg + i % vg : i;
-            t.x += sums[at].x;
-            t.y += sums[at].y;
+        for (int i = lane; i < per; i += 32) {
+            t.x += chan[g * per + i];
+            t.y += chan[groups * per + g * per + i];
         }
         t = warp_sum(t);
         if (lane == 0) {
-            float *to = a.part + ((p.b * a.groups + p.g0 + g) * a.slabs + blockIdx.x) * 2;
+            float *to = a.part + ((p.b * a.groups + p.c0 / a.cg + g) * a.slabs + blockIdx.x) * 2;
             to[0] = t.x;
             to[1] = t.y;
         }
     }
 }
 
-// One warp per (batch entry, group): joins the slabs.
+// One block per (batch entry, group): joins the slabs.
 template <typename T>
 __global__ void __launch_bounds__(128) norm_join_kernel(NormArgs a)
 {
     dependent_launch_enter();
-    const long long id = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    if (id >= a.batch * a.groups) return;
-    const int lane = threadIdx.x & 31;
-    const float *from = a.part + id * a.slabs * 2;
+    __shared__ float2 sums[4];
+    const long long id = blockIdx.x;
+    const float2 *from = reinterpret_cast<const float2 *>(a.part) + id * a.slabs;
     float2 s = make_float2(0.0f, 0.0f);
-    for (int i = lane; i < a.slabs; i += 32) {
-        s.x += from[2 * i];
-        s.y += from[2 * i + 1];
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.slabs; i += 128) {
+        const float2 v = from[i];
+        s.x += v.x;
+        s.y += v.y;
     }
     s = warp_sum(s);
-    if (lane == 0) {
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s.x = (sums[0].x + sums[1].x) + (sums[2].x + sums[3].x);
+        s.y = (sums[0].y + sums[1].y) + (sums[2].y + sums[3].y);
         const long long b = id / a.groups;
         const int g = static_cast<int>(id - b * a.groups);
         const float inv = 1.0f / (static_cast<float>(a.space) * static_cast<float>(a.cg));
@@ -297,54 +366,42 @@ __global__ void __launch_bounds__(kNormThreads) norm_apply_kernel(NormArgs a)
     dependent_launch_enter();
     const SlabPlace p = slab_place<V>(a, a.slabs - 1 - blockIdx.x);
     if (!p.live) return;
-    constexpr int UN = BACK ? 2 : 4;
     for (int cv = p.cv; cv < p.per_row; cv += kNormThreads) {
-        const int c = p.g0 * a.cg + cv * V;
-        const long long bg = p.b * a.groups + c / a.cg;
-        const float mean = a.mean[bg], rstd = a.rstd[bg];
-        const float m1 = BACK ? a.group_sums[2 * bg] : 0.0f, m2 = BACK ? a.group_sums[2 * bg + 1] : 0.0f;
-        float w[V], bias[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            w[j] = a.w ? a.w[c + j] : 1.0f;
-            bias[j] = a.b ? a.b[c + j] : 0.0f;
-        }
-        auto one = [&](const Pack<T, V> &x, const Pack<T, V> &dy) {
-            float out[V];
+        const int c = p.c0 + cv * V;
+        const long long bg = p.b * a.groups;
+        const Vec<V> minus = splat<V>(-1.0f);
+        const Vec<V> mean = mul2(per_channel<T, V>(c, a.cg, a.mean + bg), minus), rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
+        const Vec<V> w = mul2(load_params<float, V>(a.w, c, true, false, 1.0f), rstd), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
+        Vec<V> k1, k2;                                                   // rstd mean(p), rstd^2 mean(p xhat), negated
+        if (BACK) {
+            float f[V], h[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float xh = (x.get(j) - mean) * rstd;
-                const float v = fmaf(xh, w[j], bias[j]);
-                if (BACK) {
-                    float e = dy.get(j);
-                    if (a.silu) e *= silu_slope(v, sigmoid(v));
-                    out[j] = rstd * (fmaf(e, w[j], -m1) - xh * m2);
-                } else {
-                    out[j] = a.silu ? silu(v) : v;
-                }
+                f[j] = -a.group_sums[2 * (bg + (c + j) / a.cg)];
+                h[j] = -a.group_sums[2 * (bg + (c + j) / a.cg) + 1];
             }
-            return pack<T, V>(out);
-        };
-        long long row = p.row0 + p.r0;
+            k1 = mul2(each<V>([&](int i) { return pair(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.0f); }), rstd);
+            k2 = mul2(mul2(each<V>([&](int i) { return pair(h[2 * i], 2 * i + 1 < V ? h[2 * i + 1] : 0.0f); }), rstd), rstd);
+        }
+        const long long row = p.row0 + p.r0;
         const Tokens &to = BACK ? a.dx : a.y;
-        const T *src = norm_at<T>(a.x, p.b, row, c), *dsrc = BACK ? norm_at<T>(a.dy, p.b, row, c) : nullptr;
         T *dst = norm_at<T>(to, p.b, row, c);
-        const long long sx = p.step * a.x.tstride, sd = BACK ? p.step * a.dy.tstride : 0, so = p.step * to.tstride;
-        for (; row + (UN - 1) * p.step < p.row1; row += UN * p.step, src += UN * sx, dsrc += UN * sd, dst += UN * so) {
-            Pack<T, V> x[UN], dy[UN];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                x[u] = load_pack<T, V>(src + u * sx);
-                if (BACK) dy[u] = load_pack<T, V>(dsrc + u * sd);
-            }
-#pragma unroll
-            for (int u = 0; u < UN; ++u) store_pack(dst + u * so, one(x[u], dy[u]));
-        }
-        for (; row < p.row1; row += p.step, src += sx, dsrc += sd, dst += so) {
-            Pack<T, V> dy;
-            if (BACK) dy = load_pack<T, V>(dsrc);
-            store_pack(dst, one(load_pack<T, V>(src), dy));
-        }
+        const long long so = p.step * to.tstride;
+        walk_rows<T, V, BACK ? 2 : 4, BACK>(
+            p, norm_at<T>(a.x, p.b, row, c), p.step * a.x.tstride, BACK ? norm_at<T>(a.dy, p.b, row, c) : nullptr,
+            BACK ? p.step * a.dy.tstride : 0, [&](const Vec<V> &x, const Vec<V> &dy) {
+                const Vec<V> xm = add2(x, mean);
+                Vec<V> v = fma2(xm, w, bias);
+                if (BACK) {
+                    Vec<V> e = dy;
+                    if (a.silu) e = mul2(e, silu_slope2(v));
+                    v = fma2(e, w, fma2(xm, k2, k1));
+                } else if (a.silu) {
+                    v = silu2(v);
+                }
+                store_pack(dst, narrow<T, V>(v));
+                dst += so;
+            });
     }
 }
 
@@ -354,77 +411,43 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_stats_kernel(NormArgs 
 {
     dependent_launch_enter();
     const SlabPlace p = slab_place<V>(a, blockIdx.x);
-    __shared__ float sums[2 * V][kNormThreads];
+    __shared__ float sums[2 * V][kNormThreads], chan[2 * V * kNormThreads];
+    float *to = a.part + (p.b * a.slabs + blockIdx.x) * 2 * a.channels;
     for (int cv = p.cv; cv < (p.walk ? p.cv + 1 : p.per_row); cv += kNormThreads) {
-        float s1[V], s2[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) s1[j] = s2[j] = 0.0f;
-        const int c = p.g0 * a.cg + (p.live ? cv : 0) * V;
+        Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
+        const int c = p.c0 + (p.live ? cv : 0) * V;
         if (p.live) {
-            const long long bg = p.b * a.groups + c / a.cg;
-            const float mean = a.mean[bg], rstd = a.rstd[bg];
-            float w[V], bias[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                w[j] = a.w ? a.w[c + j] : 1.0f;
-                bias[j] = a.b ? a.b[c + j] : 0.0f;
-            }
-            constexpr int UN = 2;
-            long long row = p.row0 + p.r0;
-            const T *src = norm_at<T>(a.x, p.b, row, c), *dsrc = norm_at<T>(a.dy, p.b, row, c);
-            const long long sx = p.step * a.x.tstride, sd = p.step * a.dy.tstride;
-            auto add = [&](const Pack<T, V> &x, const Pack<T, V> &dy) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float xh = (x.get(j) - mean) * rstd;
-                    float e = dy.get(j);
-                    if (a.silu) {
-                        const float v = fmaf(xh, w[j], bias[j]);
-                        e *= silu_slope(v, sigmoid(v));
-                    }
-                    s1[j] += e;
-                    s2[j] = fmaf(e, xh, s2[j]);
-                }
-            };
-            for (; row + (UN - 1) * p.step < p.row1; row += UN * p.step, src += UN * sx, dsrc += UN * sd) {
-                Pack<T, V> x[UN], dy[UN];
-#pragma unroll
-                for (int u = 0; u < UN; ++u) {
-                    x[u] = load_pack<T, V>(src + u * sx);
-                    dy[u] = load_pack<T, V>(dsrc + u * sd);
-                }
-#pragma unroll
-                for (int u = 0; u < UN; ++u) add(x[u], dy[u]);
-            }
-            for (; row < p.row1; row += p.step, src += sx, dsrc += sd) add(load_pack<T, V>(src), load_pack<T, V>(dsrc));
+            const long long bg = p.b * a.groups;
+            const Vec<V> mean = mul2(per_channel<T, V>(c, a.cg, a.mean + bg), splat<V>(-1.0f)), rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
+            const Vec<V> w = mul2(load_params<float, V>(a.w, c, true, false, 1.0f), rstd), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
+            const long long row = p.row0 + p.r0;
+            walk_rows<T, V, 2, true>(p, norm_at<T>(a.x, p.b, row, c), p.step * a.x.tstride, norm_at<T>(a.dy, p.b, row, c), p.step * a.dy.tstride,
+                                     [&](const Vec<V> &x, const Vec<V> &dy) {
+                                         const Vec<V> xm = add2(x, mean);
+                                         Vec<V> e = dy;
+                                         if (a.silu) e = mul2(e, silu_slope2(fma2(xm, w, bias)));
+                                         s1 = add2(s1, e);
+                                         s2 = fma2(e, xm, s2);
+                                     });
+            s2 = mul2(s2, rstd);
         }
-        float *to = a.part + (p.b * a.slabs + blockIdx.x) * 2 * a.channels;
         if (!p.walk) {                                                   // a channel belongs to one thread
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                to[c + j] = s1[j];
-                to[a.channels + c + j] = s2[j];
+                to[c + j] = s1.get(j);
+                to[a.channels + c + j] = s2.get(j);
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                sums[j][threadIdx.x] = s1[j];
-                sums[V + j][threadIdx.x] = s2[j];
-            }
-            __syncthreads();
-            for (int q = threadIdx.x; q < 2 * V * p.per_row; q += kNormThreads) {
-                const int which = q / (V * p.per_row), ch = q - which * V * p.per_row;
-                float v = 0.0f;
-                for (int r = 0; r < p.step; ++r) v += sums[which * V + ch % V][r * p.per_row + ch / V];
-                to[which * a.channels + p.g0 * a.cg + ch] = v;
-            }
+            add_rows<V>(p, s1, s2, sums, chan);
+            for (int q = threadIdx.x; q < 2 * p.channels; q += kNormThreads)
+                to[q / p.channels * a.channels + p.c0 + q % p.channels] = chan[q];
         }
     }
 }
 
 // Joins the slabs of one batch entry and a few groups: per channel sums for dw and db, and the groups' means of p and
 // p xhat.  The block's threads are channels x slab lanes.
-constexpr int kJoinChannels = 64;        // channels per block, unless one group has more
+constexpr int kJoinChannels = 16;        // channels per block, unless one group has more
 
 __global__ void __launch_bounds__(kNormThreads) norm_back_join_kernel(NormArgs a)
 {
@@ -533,7 +556,7 @@ __global__ void __launch_bounds__(1024) norm_param_kernel(const float *pq, long 
 
 struct NormPlan {
     int v, r;                    // channels per access, vectors per lane (warp form; 0: slabs)
-    int tile_groups, tiles, rows_per_slab, slabs, entry_step;
+    int tile, tiles, rows_per_slab, slabs, entry_step;
     long long part_floats, pq_floats, sum_floats, stat_floats;
 };
 
@@ -542,11 +565,15 @@ NormPlan norm_plan(const sysgroupnorm_args &a, bool back)
     NormPlan p = {};
     const size_t esz = a.type == SYSCONV_T_F32 ? 4 : 2;
     const long long cg = a.channels / a.groups;
-    p.v = static_cast<int>(16 / esz);
-    while (p.v > 1 && (cg % p.v != 0 || !rows_aligned(a.x, false, esz, p.v * esz) ||
-                       (back ? !rows_aligned(a.dy, false, esz, p.v * esz) || !rows_aligned(a.dx, false, esz, p.v * esz)
-                             : !rows_aligned(a.y, false, esz, p.v * esz))))
-        p.v /= 2;
+    const int widest = static_cast<int>(16 / esz);
+    auto aligned = [&](long long v) {
+        const size_t bytes = v * esz;
+        return rows_aligned(a.x, false, esz, bytes) && (back ? rows_aligned(a.dy, false, esz, bytes) && rows_aligned(a.dx, false, esz, bytes)
+                                                             : rows_aligned(a.y, false, esz, bytes));
+    };
+    // a warp per group: its vectors lie inside the group
+    p.v = widest;
+    while (p.v > 1 && (cg % p.v != 0 || !aligned(p.v))) p.v /= 2;
     const long long vectors = a.space * (cg / p.v);
     const int most = back ? 2 : 4;                                       // vectors per lane
     if (vectors <= 32 * most && (!back || a.space == 1)) {
@@ -558,13 +585,19 @@ NormPlan norm_plan(const sysgroupnorm_args &a, bool back)
         if (back) p.pq_floats = 2LL * p.entry_step * a.channels;
         return p;
     }
-    const long long vg = cg / p.v;
-    long long tg = vg > kNormThreads ? 1 : kNormThreads / vg;
-    if (tg > a.groups) tg = a.groups;
-    p.tile_groups = static_cast<int>(tg);
-    p.tiles = ceil_div(a.groups, tg);
-    // enough slabs for eight blocks an SM, at least 16 rows per thread in a slab
-    const long long per_row = tg * vg, step = per_row <= kNormThreads ? kNormThreads / per_row : 1;
+    // slabs: a tile is all channels if a row of them has at most 256 vectors, else as many whole groups as do
+    const int inside = p.v;
+    p.v = widest;
+    while (p.v > 1 && (a.channels % p.v != 0 || !aligned(p.v))) p.v /= 2;
+    long long tile = a.channels;
+    if (a.channels > kNormThreads * p.v) {
+        p.v = inside;
+        tile = cg > kNormThreads * p.v ? cg : kNormThreads * p.v / cg * cg;
+    }
+    p.tile = static_cast<int>(tile);
+    p.tiles = ceil_div(a.channels, tile);
+    // two waves of eight blocks an SM, at least eight rows per thread in a slab
+    const long long per_row = tile / p.v, step = per_row <= kNormThreads ? kNormThreads / per_row : 1;
     long long slabs = 148LL * 16 / (a.batch * p.tiles);
     if (slabs < 1) slabs = 1;
     const long long most_slabs = (a.space + 8 * step - 1) / (8 * step);
@@ -604,7 +637,7 @@ NormArgs norm_args(const sysgroupnorm_args &a, const NormPlan &p)
     k.cg = static_cast<int>(a.channels / a.groups);
     k.eps = static_cast<float>(a.eps);
     k.silu = a.activation == SYSCONV_ACT_SILU;
-    k.tile_groups = p.tile_groups;
+    k.tile = p.tile;
     k.rows_per_slab = p.rows_per_slab;
     k.slabs = p.slabs;
     k.entry_step = p.entry_step;
@@ -690,7 +723,7 @@ cudaError_t launch_groupnorm(const sysgroupnorm_args &a, cudaStream_t s, int *la
                 q.part = k.part + b0 * k.groups * k.slabs * 2;
                 const dim3 grid(p.slabs, p.tiles, static_cast<unsigned>(q.batch)), block(kNormThreads);
                 cudaError_t err = launch_kernel(norm_stats_kernel<T, V>, grid, block, s, q);
-                if (err == cudaSuccess) err = launch_kernel(norm_join_kernel<T>, dim3(ceil_div(q.batch * q.groups, 4)), dim3(128), s, q);
+                if (err == cudaSuccess) err = launch_kernel(norm_join_kernel<T>, dim3(static_cast<unsigned>(q.batch * q.groups)), dim3(128), s, q);
                 if (err == cudaSuccess) err = launch_kernel(norm_apply_kernel<T, V, false>, grid, block, s, q);
                 *launches += 3;
                 return err;

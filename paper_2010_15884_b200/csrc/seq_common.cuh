@@ -264,6 +264,63 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
     return r;
 }
 
+// V neighbouring channels in registers, two to a packed pair (V = 1: the upper half idles)
+template <int V>
+struct Vec {
+    static constexpr int N = (V + 1) / 2;
+    f32x2 p[N];
+    __device__ __forceinline__ float get(int i) const
+    {
+        const float2 v = halves(p[i / 2]);
+        return i & 1 ? v.y : v.x;
+    }
+};
+template <int V, typename F>
+__device__ __forceinline__ Vec<V> each(F f)                    // f(i): pair i
+{
+    Vec<V> r;
+#pragma unroll
+    for (int i = 0; i < Vec<V>::N; ++i) r.p[i] = f(i);
+    return r;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> splat(float v) { return each<V>([&](int) { return pair(v, v); }); }
+template <int V>
+__device__ __forceinline__ Vec<V> fma2(const Vec<V> &a, const Vec<V> &b, const Vec<V> &c)
+{
+    return each<V>([&](int i) { return fma2(a.p[i], b.p[i], c.p[i]); });
+}
+template <int V>
+__device__ __forceinline__ Vec<V> mul2(const Vec<V> &a, const Vec<V> &b) { return each<V>([&](int i) { return mul2(a.p[i], b.p[i]); }); }
+template <int V>
+__device__ __forceinline__ Vec<V> add2(const Vec<V> &a, const Vec<V> &b) { return each<V>([&](int i) { return add2(a.p[i], b.p[i]); }); }
+template <typename T, int V>
+__device__ __forceinline__ Vec<V> widen(const Pack<T, V> &v)
+{
+    return each<V>([&](int i) { return pair(v.get(2 * i), 2 * i + 1 < V ? v.get(2 * i + 1) : 0.0f); });
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> narrow(const Vec<V> &v)
+{
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = v.get(i);
+    return pack<T, V>(f);
+}
+// V neighbouring parameters (fp32 or T), one access where `wide`; `otherwise` where there are none
+template <typename T, int V>
+__device__ __forceinline__ Vec<V> load_params(const void *p, long long at, bool f32, bool wide, float otherwise)
+{
+    if (p == nullptr) return splat<V>(otherwise);
+    if constexpr (V > 1 && V * sizeof(float) <= 16) {
+        if (wide) return f32 ? widen(load_pack<float, V>(static_cast<const float *>(p) + at)) : widen(load_pack<T, V>(static_cast<const T *>(p) + at));
+    }
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = f32 ? static_cast<const float *>(p)[at + i] : to_f32(static_cast<const T *>(p)[at + i]);
+    return each<V>([&](int i) { return pair(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.0f); });
+}
+
 // ---- elementary functions -------------------------------------------------------------------------------------
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.92596299e-8f;   // log2(e) as two floats
 
@@ -326,6 +383,17 @@ __device__ __forceinline__ f32x2 sigmoid2(f32x2 v)
     return pair(rcp_fast(w.x), rcp_fast(w.y));
 }
 __device__ __forceinline__ f32x2 silu2(f32x2 v) { return mul2(v, sigmoid2(v)); }
+template <int V>
+__device__ __forceinline__ Vec<V> silu2(const Vec<V> &v) { return each<V>([&](int i) { return silu2(v.p[i]); }); }
+// d silu / dv = s (1 + v (1 - s)), s = 1 / (1 + exp(-v))
+template <int V>
+__device__ __forceinline__ Vec<V> silu_slope2(const Vec<V> &v)
+{
+    return each<V>([&](int i) {
+        const f32x2 s = sigmoid2(v.p[i]);
+        return mul2(s, fma2(v.p[i], fma2(s, pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), pair(1.0f, 1.0f)));
+    });
+}
 __device__ __forceinline__ float sigmoid(float v) { return rcp_fast(1.0f + exp2_fast(-kLog2e * v)); }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
 __device__ __forceinline__ float silu_slope(float v, float sig) { return sig * fmaf(v, 1.0f - sig, 1.0f); }
