@@ -35,7 +35,7 @@ struct CausalArgs {
     bool weight_f32, silu;
 };
 
-// Filter and bias of V channels from c on: w[k], the channels packed in pairs.  The V x K numbers are contiguous.
+// Filter and bias of V channels from c on.  The V x K numbers are contiguous.
 template <typename T, int V, int K>
 __device__ __forceinline__ void load_filter(const CausalArgs &a, int c, Vec<V> (&w)[K], Vec<V> &bias)
 {
@@ -48,7 +48,7 @@ __device__ __forceinline__ void load_filter(const CausalArgs &a, int c, Vec<V> (
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        w[k] = each<V>([&](int i) { return pair(f[2 * i * K + k], 2 * i + 1 < V ? f[(2 * i + 1) * K % (V * K) + k] : 0.0f); });
+        w[k] = each<V>([&](int i) { return f[i * K + k]; });
     bias = load_params<T, V>(a.bias, c, a.weight_f32, V > 1, 0.0f);
 }
 
@@ -94,13 +94,57 @@ __device__ __forceinline__ int pass_empty(const CausalArgs &a, int r, long long 
     return r;
 }
 
-constexpr int kAhead = 4;                // tokens per step of a thread; the next step's loads are in flight meanwhile
+constexpr int kAhead = 4;                // tokens per step of a thread
+
+// A thread's input rows, kAhead at a time, STAGES - 1 steps ahead in its own part of shared memory (types and widths that
+// asynchronous copies do not have are loaded when they are needed).
+template <typename T, int V, int THREADS, int STAGES>
+struct Stream {
+    static constexpr int BYTES = V * static_cast<int>(sizeof(T));
+    static constexpr bool ASYNC = BYTES >= 4;
+    static constexpr int SLOTS = ASYNC ? STAGES * kAhead : 0;
+    struct alignas(16) Room {
+        char at[SLOTS > 0 ? SLOTS : 1][THREADS][ASYNC ? BYTES : 1];
+    };
+    Room *room;
+    int thread;
+    const T *src;
+    long long stride;
+    int in, out;                                                    // next slot to fill, next slot to read
+    __device__ __forceinline__ Stream(Room *r, int th, const T *s, long long st) : room(r), thread(th), src(s), stride(st), in(0), out(0) {}
+    __device__ __forceinline__ void fill(bool wanted)              // kAhead rows, without the commit
+    {
+        if constexpr (ASYNC) {
+            if (wanted)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) copy_async<BYTES>(room->at[in + u][thread], src + u * stride);
+            in = in + kAhead == SLOTS ? 0 : in + kAhead;
+            src += kAhead * stride;
+        }
+    }
+    __device__ __forceinline__ void take(Pack<T, V> (&raw)[kAhead])
+    {
+        if constexpr (ASYNC) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) raw[u] = load_pack<T, V>(reinterpret_cast<const T *>(room->at[out + u][thread]));
+            out = out + kAhead == SLOTS ? 0 : out + kAhead;
+        } else {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) raw[u] = load_pack<T, V>(src + u * stride);
+            src += kAhead * stride;
+        }
+    }
+};
+template <typename T, int V>
+struct Stages { static constexpr int value = V * sizeof(T) <= 8 ? 4 : 2; };
 
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
 {
     dependent_launch_enter();
-    constexpr int U = kAhead;
+    constexpr int U = kAhead, STAGES = Stages<T, V>::value;
+    using In = Stream<T, V, kThreads, STAGES>;
+    __shared__ typename In::Room room;
     const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     const long long run = id / a.groups;
     if (run >= a.runs) return;
@@ -119,15 +163,16 @@ __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
         const T *src = token_row<T>(a.x, a.map, r, t) + c;
         T *dst = token_row<T>(a.y, a.map, r, t) + c;
         const long long xs = a.x.tstride, ys = a.y.tstride;
-        if (left > 0) t += left;
+        if (left < 0) left = 0;
+        t += left;
         auto outputs = [&](auto count) {
             constexpr int N = decltype(count)::value;
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 Vec<V> v = bias;
 #pragma unroll
-                for (int k = 0; k < K; ++k) v = fma2(w[k], line[u + k], v);
-                if (a.silu) v = silu2(v);
+                for (int k = 0; k < K; ++k) v = vfma(w[k], line[u + k], v);
+                if (a.silu) v = vsilu(v);
                 store_pack(dst + u * ys, narrow<T, V>(v));
             }
 #pragma unroll
@@ -135,20 +180,21 @@ __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
             dst += N * ys;
             left -= N;
         };
-        Pack<T, V> raw[U];
-        if (left >= U) {
+        In rows(&room, threadIdx.x, src, xs);
+        src += left / U * U * xs;                                   // the rest, one by one
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = load_pack<T, V>(src + u * xs);
-            src += U * xs;
+        for (int i = 0; i < STAGES - 1; ++i) {
+            rows.fill(left >= (i + 1) * U);
+            copy_commit();
         }
         while (left >= U) {
+            copy_wait<STAGES - 2>();
+            Pack<T, V> raw[U];
+            rows.take(raw);
 #pragma unroll
             for (int u = 0; u < U; ++u) line[K - 1 + u] = widen(raw[u]);
-            if (left >= 2 * U) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) raw[u] = load_pack<T, V>(src + u * xs);
-                src += U * xs;
-            }
+            rows.fill(left >= STAGES * U);
+            copy_commit();
             outputs(Count<U>{});
         }
         while (left > 0) {
@@ -175,7 +221,13 @@ template <typename T, int V, int K>
 __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalArgs a)
 {
     dependent_launch_enter();
-    constexpr int U = kAhead;
+    constexpr int U = kAhead, STAGES = Stages<T, V>::value;
+    using In = Stream<T, V, 32 * kBackRows, STAGES>;
+    using Sums = float[kBackRows][(K + 1) * V][33];
+    constexpr size_t ROOM = 2 * sizeof(typename In::Room) > sizeof(Sums) ? 2 * sizeof(typename In::Room) : sizeof(Sums);
+    __shared__ __align__(16) char shared[ROOM];                      // the rows on their way in, then the block's sums
+    typename In::Room *room = reinterpret_cast<typename In::Room *>(shared);
+    const int tid = threadIdx.y * 32 + threadIdx.x;
     const int group = blockIdx.x * 32 + threadIdx.x;
     const long long run = static_cast<long long>(blockIdx.y) * kBackRows + threadIdx.y;
     const bool live = group < a.groups && run < a.runs;
@@ -192,7 +244,7 @@ __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalA
         // dL/dline row s of sequence r (s before `first`: its state): f, and what comes through the final state
         auto emit = [&](int rr, long long first, long long end, long long s, Vec<V> f) {
             if (a.dfinal != nullptr && s >= end - (K - 1))
-                f = add2(f, widen(load_pack<T, V>(static_cast<const T *>(a.dfinal) +
+                f = vadd(f, widen(load_pack<T, V>(static_cast<const T *>(a.dfinal) +
                                                   (static_cast<long long>(rr) * (K - 1) + (s - end + K - 1)) * a.channels + c)));
             if (s >= first) {
                 if (a.dx.ptr != nullptr) store_pack(token_row<T>(a.dx, a.map, rr, s) + c, narrow<T, V>(f));
@@ -226,19 +278,19 @@ __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalA
                 if (!a.silu) return dy;
                 Vec<V> v = bias;
 #pragma unroll
-                for (int k = 0; k < K; ++k) v = fma2(w[k], line[u + k], v);
-                return mul2(dy, silu_slope2(v));
+                for (int k = 0; k < K; ++k) v = vfma(w[k], line[u + k], v);
+                return vmul(dy, vsilu_slope(v));
             };
             auto gather = [&](int u) {                               // dL/dline of the oldest token in g[u ..]
-                Vec<V> f = mul2(w[0], g[u + K - 1]);
+                Vec<V> f = vmul(w[0], g[u + K - 1]);
 #pragma unroll
-                for (int k = 1; k < K; ++k) f = fma2(w[k], g[u + K - 1 - k], f);
+                for (int k = 1; k < K; ++k) f = vfma(w[k], g[u + K - 1 - k], f);
                 return f;
             };
             auto accumulate = [&](int u) {
-                db = add2(db, g[u + K - 1]);
+                db = vadd(db, g[u + K - 1]);
 #pragma unroll
-                for (int k = 0; k < K; ++k) dw[k] = fma2(g[u + K - 1], line[u + k], dw[k]);
+                for (int k = 0; k < K; ++k) dw[k] = vfma(g[u + K - 1], line[u + k], dw[k]);
             };
             auto one = [&]() {
                 if (t < last) {
@@ -261,30 +313,31 @@ __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalA
             // rows before the first of this run's tokens
             for (int k = 0; k < K - 1 && t < flush; ++k) one();
             T *out = a.dx.ptr != nullptr ? token_row<T>(a.dx, a.map, r, t - (K - 1)) + c : nullptr;
-            if (t + U <= mine) {
-                Pack<T, V> xr[U], yr[U];
+            int steps = t + U <= mine ? static_cast<int>((mine - t) / U) : 0;
+            if (steps > 0) {
+                In xrows(&room[0], tid, src, xs), yrows(&room[1], tid, dsrc, ys);
+                t += steps * U;
+                src += steps * U * xs;
+                dsrc += steps * U * ys;
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    xr[u] = load_pack<T, V>(src + u * xs);
-                    yr[u] = load_pack<T, V>(dsrc + u * ys);
+                for (int i = 0; i < STAGES - 1; ++i) {
+                    xrows.fill(steps > i);
+                    yrows.fill(steps > i);
+                    copy_commit();
                 }
-                while (t + U <= mine) {
+                for (; steps > 0; --steps) {
+                    copy_wait<STAGES - 2>();
+                    Pack<T, V> raw[U];
                     Vec<V> dy[U];
+                    xrows.take(raw);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        line[K - 1 + u] = widen(xr[u]);
-                        dy[u] = widen(yr[u]);
-                    }
-                    t += U;
-                    src += U * xs;
-                    dsrc += U * ys;
-                    if (t + U <= mine) {
+                    for (int u = 0; u < U; ++u) line[K - 1 + u] = widen(raw[u]);
+                    yrows.take(raw);
 #pragma unroll
-                        for (int u = 0; u < U; ++u) {
-                            xr[u] = load_pack<T, V>(src + u * xs);
-                            yr[u] = load_pack<T, V>(dsrc + u * ys);
-                        }
-                    }
+                    for (int u = 0; u < U; ++u) dy[u] = widen(raw[u]);
+                    xrows.fill(steps >= STAGES);
+                    yrows.fill(steps >= STAGES);
+                    copy_commit();
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         g[K - 1 + u] = slope_of(u, dy[u]);
@@ -305,7 +358,9 @@ __global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalA
         }
     }
     if (a.partial == nullptr) return;
-    __shared__ float sums[kBackRows][(K + 1) * V][33];
+    copy_wait<0>();
+    __syncthreads();                                                // every thread's rows have been used
+    Sums &sums = *reinterpret_cast<Sums *>(shared);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll

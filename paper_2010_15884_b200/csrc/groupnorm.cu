@@ -110,10 +110,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
             Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const Vec<V> v = add2(x[i], splat<V>(ok[i] ? -shift : -x[i].get(0)));
+                const Vec<V> v = vadd(x[i], splat<V>(ok[i] ? -shift : -x[i].get(0)));
                 if (ok[i]) {
-                    s1 = add2(s1, v);
-                    s2 = fma2(v, v, s2);
+                    s1 = vadd(s1, v);
+                    s2 = vfma(v, v, s2);
                 }
             }
             float2 s = make_float2(0.0f, 0.0f);
@@ -131,8 +131,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
             }
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                Vec<V> v = fma2(add2(x[i], splat<V>(-mean)), mul2(wv[i], splat<V>(rstd)), bv[i]);
-                if (a.silu) v = silu2(v);
+                Vec<V> v = vfma(vadd(x[i], splat<V>(-mean)), vmul(wv[i], splat<V>(rstd)), bv[i]);
+                if (a.silu) v = vsilu(v);
                 if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(v));
             }
         } else {
@@ -140,14 +140,14 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
             Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                x[i] = mul2(add2(x[i], splat<V>(-mean)), splat<V>(rstd));
-                if (a.silu) e[i] = mul2(e[i], silu_slope2(fma2(x[i], wv[i], bv[i])));
+                x[i] = vmul(vadd(x[i], splat<V>(-mean)), splat<V>(rstd));
+                if (a.silu) e[i] = vmul(e[i], vsilu_slope(vfma(x[i], wv[i], bv[i])));
                 if (ok[i]) {
-                    db[i] = add2(db[i], e[i]);
-                    dw[i] = fma2(e[i], x[i], dw[i]);
-                    e[i] = mul2(e[i], wv[i]);
-                    s1 = add2(s1, e[i]);
-                    s2 = fma2(e[i], x[i], s2);
+                    db[i] = vadd(db[i], e[i]);
+                    dw[i] = vfma(e[i], x[i], dw[i]);
+                    e[i] = vmul(e[i], wv[i]);
+                    s1 = vadd(s1, e[i]);
+                    s2 = vfma(e[i], x[i], s2);
                 }
             }
             float2 s = make_float2(0.0f, 0.0f);
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
             const Vec<V> m1 = splat<V>(-s.x * inv), m2 = splat<V>(-s.y * inv);
 #pragma unroll
             for (int i = 0; i < R; ++i)
-                if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(mul2(splat<V>(rstd), add2(fma2(x[i], m2, m1), e[i]))));
+                if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(vmul(splat<V>(rstd), vadd(vfma(x[i], m2, m1), e[i]))));
         }
         po += a.entry_step * out_t.bstride;
     }
@@ -206,54 +206,68 @@ __device__ __forceinline__ SlabPlace slab_place(const NormArgs &a, int slab)
     return p;
 }
 
-// f(packs of rows u = 0 .. n-1) over this thread's rows, UN at a time with the next ones' loads in flight, then one by one
-template <typename T, int V, int UN, bool TWO, typename F>
-__device__ __forceinline__ void walk_rows(const SlabPlace &p, const T *x, long long sx, const T *y, long long sy, F f)
+// A block's shared memory: the threads' rows on their way in, then their sums.
+constexpr int kRoom = 32 * 1024;
+template <typename T, int V, bool TWO>
+struct RowRing {
+    static constexpr int BYTES = V * static_cast<int>(sizeof(T)), STREAMS = TWO ? 2 : 1;
+    static constexpr bool ASYNC = BYTES >= 4;
+    static constexpr int DEPTH = ASYNC ? kRoom / (kNormThreads * BYTES * STREAMS) < 16 ? kRoom / (kNormThreads * BYTES * STREAMS) : 16 : 1;
+    static_assert(DEPTH >= 1, "room for a row");
+};
+
+// f(row of x, row of y) for each of this thread's rows; asynchronous copies run DEPTH - 1 rows ahead
+template <typename T, int V, bool TWO, typename F>
+__device__ __forceinline__ void walk_rows(const SlabPlace &p, char *room, const T *x, long long sx, const T *y, long long sy, F f)
 {
-    long long left = p.row1 - (p.row0 + p.r0);
-    int n = left <= 0 ? 0 : static_cast<int>((left + p.step - 1) / p.step);
-    Pack<T, V> a[UN], b[TWO ? UN : 1];
-    auto load = [&](int count) {
+    using G = RowRing<T, V, TWO>;
+    constexpr int BYTES = G::BYTES, DEPTH = G::DEPTH;
+    const long long left = p.row1 - (p.row0 + p.r0);
+    const int n = left <= 0 ? 0 : static_cast<int>((left + p.step - 1) / p.step);
+    if constexpr (!G::ASYNC) {
+        for (int i = 0; i < n; ++i, x += sx, y += TWO ? sy : 0)
+            f(widen(load_pack<T, V>(x)), widen(load_pack<T, V>(TWO ? y : x)));
+    } else {
+        char *own = room + threadIdx.x * BYTES;                          // slot s of stream k at (s * STREAMS + k) * threads
+        constexpr int PITCH = kNormThreads * BYTES, SLOT = PITCH * G::STREAMS;
+        const T *nx = x, *ny = y;
 #pragma unroll
-        for (int u = 0; u < UN; ++u)
-            if (u < count) {
-                a[u] = load_pack<T, V>(x + u * sx);
-                if (TWO) b[u] = load_pack<T, V>(y + u * sy);
+        for (int i = 0; i < DEPTH - 1; ++i) {
+            if (i < n) {
+                copy_async<BYTES>(own + i * SLOT, nx);
+                if (TWO) copy_async<BYTES>(own + i * SLOT + PITCH, ny);
+                nx += sx;
+                if (TWO) ny += sy;
             }
-        x += UN * sx;
-        if (TWO) y += UN * sy;
-    };
-    if (n >= UN) load(UN);
-    while (n >= UN) {
-        Vec<V> va[UN], vb[TWO ? UN : 1];
-#pragma unroll
-        for (int u = 0; u < UN; ++u) {
-            va[u] = widen(a[u]);
-            if (TWO) vb[u] = widen(b[u]);
+            copy_commit();
         }
-        n -= UN;
-        if (n >= UN) load(UN);
-#pragma unroll
-        for (int u = 0; u < UN; ++u) f(va[u], vb[TWO ? u : 0]);
-    }
-    while (n > 0) {
-        const Vec<V> va = widen(load_pack<T, V>(x));
-        Vec<V> vb;
-        if (TWO) vb = widen(load_pack<T, V>(y));
-        f(va, vb);
-        x += sx;
-        if (TWO) y += sy;
-        --n;
+        int slot = 0, ahead = DEPTH - 1;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            copy_wait<DEPTH - 2>();
+            const char *at = own + slot * SLOT;
+            const Pack<T, V> a = load_pack<T, V>(reinterpret_cast<const T *>(at));
+            Pack<T, V> b = a;
+            if (TWO) b = load_pack<T, V>(reinterpret_cast<const T *>(at + PITCH));
+            if (i + DEPTH - 1 < n) {
+                copy_async<BYTES>(own + ahead * SLOT, nx);
+                if (TWO) copy_async<BYTES>(own + ahead * SLOT + PITCH, ny);
+                nx += sx;
+                if (TWO) ny += sy;
+            }
+            copy_commit();
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
+            ahead = ahead + 1 == DEPTH ? 0 : ahead + 1;
+            f(widen(a), widen(b));
+        }
+        copy_wait<0>();
     }
 }
 
 template <typename T, int V>
 __device__ __forceinline__ Vec<V> per_channel(int c, int cg, const float *from)      // from[group of channel]
 {
-    float f[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = from[(c + j) / cg];
-    return each<V>([&](int i) { return pair(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.0f); });
+    return each<V>([&](int j) { return from[(c + j) / cg]; });
 }
 
 // Per channel sums of a block's threads: s1 and s2 over the threads that share a vector, into chan[2][channels of the tile].
@@ -280,24 +294,24 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs a)
 {
     dependent_launch_enter();
     const SlabPlace p = slab_place<V>(a, blockIdx.x);
-    __shared__ float sums[2 * V][kNormThreads], chan[2 * V * kNormThreads];
+    __shared__ __align__(16) char room[kRoom];
+    static_assert(4 * V * kNormThreads * sizeof(float) <= kRoom, "room for the sums");
+    float (*sums)[kNormThreads] = reinterpret_cast<float (*)[kNormThreads]>(room), *chan = sums[2 * V];
     Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
     if (p.live)
         for (int cv = p.cv; cv < p.per_row; cv += kNormThreads) {        // once in the walking form
             const int c = p.c0 + cv * V;
-            float k[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) k[j] = -to_f32(*norm_at<T>(a.x, p.b, 0, (c + j) / a.cg * a.cg));
-            const Vec<V> shift = each<V>([&](int i) { return pair(k[2 * i], 2 * i + 1 < V ? k[2 * i + 1] : 0.0f); });
-            walk_rows<T, V, 4, false>(p, norm_at<T>(a.x, p.b, p.row0 + p.r0, c), p.step * a.x.tstride, static_cast<const T *>(nullptr), 0,
+            const Vec<V> shift = each<V>([&](int j) { return -to_f32(*norm_at<T>(a.x, p.b, 0, (c + j) / a.cg * a.cg)); });
+            walk_rows<T, V, false>(p, room, norm_at<T>(a.x, p.b, p.row0 + p.r0, c), p.step * a.x.tstride, static_cast<const T *>(nullptr), 0,
                                       [&](const Vec<V> &x, const Vec<V> &) {
-                                          const Vec<V> v = add2(x, shift);
-                                          s1 = add2(s1, v);
-                                          s2 = fma2(v, v, s2);
+                                          const Vec<V> v = vadd(x, shift);
+                                          s1 = vadd(s1, v);
+                                          s2 = vfma(v, v, s2);
                                       });
         }
     // groups of the tile, one warp each: their channels' sums, or (one wide group) every thread's
     int per = a.cg, groups = p.channels / a.cg;
+    __syncthreads();                                                     // every thread's rows have been used
     if (p.walk) {
         add_rows<V>(p, s1, s2, sums, chan);
     } else {
@@ -365,39 +379,34 @@ __global__ void __launch_bounds__(kNormThreads) norm_apply_kernel(NormArgs a)
 {
     dependent_launch_enter();
     const SlabPlace p = slab_place<V>(a, a.slabs - 1 - blockIdx.x);
+    __shared__ __align__(16) char room[kRoom];
     if (!p.live) return;
     for (int cv = p.cv; cv < p.per_row; cv += kNormThreads) {
         const int c = p.c0 + cv * V;
         const long long bg = p.b * a.groups;
         const Vec<V> minus = splat<V>(-1.0f);
-        const Vec<V> mean = mul2(per_channel<T, V>(c, a.cg, a.mean + bg), minus), rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
-        const Vec<V> w = mul2(load_params<float, V>(a.w, c, true, false, 1.0f), rstd), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
+        const Vec<V> mean = vmul(per_channel<T, V>(c, a.cg, a.mean + bg), minus), rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
+        const Vec<V> w = vmul(load_params<float, V>(a.w, c, true, false, 1.0f), rstd), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
         Vec<V> k1, k2;                                                   // rstd mean(p), rstd^2 mean(p xhat), negated
         if (BACK) {
-            float f[V], h[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                f[j] = -a.group_sums[2 * (bg + (c + j) / a.cg)];
-                h[j] = -a.group_sums[2 * (bg + (c + j) / a.cg) + 1];
-            }
-            k1 = mul2(each<V>([&](int i) { return pair(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.0f); }), rstd);
-            k2 = mul2(mul2(each<V>([&](int i) { return pair(h[2 * i], 2 * i + 1 < V ? h[2 * i + 1] : 0.0f); }), rstd), rstd);
+            k1 = vmul(each<V>([&](int j) { return -a.group_sums[2 * (bg + (c + j) / a.cg)]; }), rstd);
+            k2 = vmul(vmul(each<V>([&](int j) { return -a.group_sums[2 * (bg + (c + j) / a.cg) + 1]; }), rstd), rstd);
         }
         const long long row = p.row0 + p.r0;
         const Tokens &to = BACK ? a.dx : a.y;
         T *dst = norm_at<T>(to, p.b, row, c);
         const long long so = p.step * to.tstride;
-        walk_rows<T, V, BACK ? 2 : 4, BACK>(
-            p, norm_at<T>(a.x, p.b, row, c), p.step * a.x.tstride, BACK ? norm_at<T>(a.dy, p.b, row, c) : nullptr,
+        walk_rows<T, V, BACK>(
+            p, room, norm_at<T>(a.x, p.b, row, c), p.step * a.x.tstride, BACK ? norm_at<T>(a.dy, p.b, row, c) : nullptr,
             BACK ? p.step * a.dy.tstride : 0, [&](const Vec<V> &x, const Vec<V> &dy) {
-                const Vec<V> xm = add2(x, mean);
-                Vec<V> v = fma2(xm, w, bias);
+                const Vec<V> xm = vadd(x, mean);
+                Vec<V> v = vfma(xm, w, bias);
                 if (BACK) {
                     Vec<V> e = dy;
-                    if (a.silu) e = mul2(e, silu_slope2(v));
-                    v = fma2(e, w, fma2(xm, k2, k1));
+                    if (a.silu) e = vmul(e, vsilu_slope(v));
+                    v = vfma(e, w, vfma(xm, k2, k1));
                 } else if (a.silu) {
-                    v = silu2(v);
+                    v = vsilu(v);
                 }
                 store_pack(dst, narrow<T, V>(v));
                 dst += so;
@@ -411,25 +420,27 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_stats_kernel(NormArgs 
 {
     dependent_launch_enter();
     const SlabPlace p = slab_place<V>(a, blockIdx.x);
-    __shared__ float sums[2 * V][kNormThreads], chan[2 * V * kNormThreads];
+    __shared__ __align__(16) char room[kRoom];
+    static_assert(4 * V * kNormThreads * sizeof(float) <= kRoom, "room for the sums");
+    float (*sums)[kNormThreads] = reinterpret_cast<float (*)[kNormThreads]>(room), *chan = sums[2 * V];
     float *to = a.part + (p.b * a.slabs + blockIdx.x) * 2 * a.channels;
     for (int cv = p.cv; cv < (p.walk ? p.cv + 1 : p.per_row); cv += kNormThreads) {
         Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
         const int c = p.c0 + (p.live ? cv : 0) * V;
         if (p.live) {
             const long long bg = p.b * a.groups;
-            const Vec<V> mean = mul2(per_channel<T, V>(c, a.cg, a.mean + bg), splat<V>(-1.0f)), rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
-            const Vec<V> w = mul2(load_params<float, V>(a.w, c, true, false, 1.0f), rstd), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
+            const Vec<V> mean = vmul(per_channel<T, V>(c, a.cg, a.mean + bg), splat<V>(-1.0f)), rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
+            const Vec<V> w = vmul(load_params<float, V>(a.w, c, true, false, 1.0f), rstd), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
             const long long row = p.row0 + p.r0;
-            walk_rows<T, V, 2, true>(p, norm_at<T>(a.x, p.b, row, c), p.step * a.x.tstride, norm_at<T>(a.dy, p.b, row, c), p.step * a.dy.tstride,
+            walk_rows<T, V, true>(p, room, norm_at<T>(a.x, p.b, row, c), p.step * a.x.tstride, norm_at<T>(a.dy, p.b, row, c), p.step * a.dy.tstride,
                                      [&](const Vec<V> &x, const Vec<V> &dy) {
-                                         const Vec<V> xm = add2(x, mean);
+                                         const Vec<V> xm = vadd(x, mean);
                                          Vec<V> e = dy;
-                                         if (a.silu) e = mul2(e, silu_slope2(fma2(xm, w, bias)));
-                                         s1 = add2(s1, e);
-                                         s2 = fma2(e, xm, s2);
+                                         if (a.silu) e = vmul(e, vsilu_slope(vfma(xm, w, bias)));
+                                         s1 = vadd(s1, e);
+                                         s2 = vfma(e, xm, s2);
                                      });
-            s2 = mul2(s2, rstd);
+            s2 = vmul(s2, rstd);
         }
         if (!p.walk) {                                                   // a channel belongs to one thread
 #pragma unroll
@@ -438,6 +449,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_stats_kernel(NormArgs 
                 to[a.channels + c + j] = s2.get(j);
             }
         } else {
+            __syncthreads();                                             // every thread's rows have been used
             add_rows<V>(p, s1, s2, sums, chan);
             for (int q = threadIdx.x; q < 2 * p.channels; q += kNormThreads)
                 to[q / p.channels * a.channels + p.c0 + q % p.channels] = chan[q];
@@ -596,9 +608,9 @@ NormPlan norm_plan(const sysgroupnorm_args &a, bool back)
     }
     p.tile = static_cast<int>(tile);
     p.tiles = ceil_div(a.channels, tile);
-    // two waves of eight blocks an SM, at least eight rows per thread in a slab
+    // two waves of four blocks an SM, at least eight rows per thread in a slab
     const long long per_row = tile / p.v, step = per_row <= kNormThreads ? kNormThreads / per_row : 1;
-    long long slabs = 148LL * 16 / (a.batch * p.tiles);
+    long long slabs = 148LL * 8 / (a.batch * p.tiles);
     if (slabs < 1) slabs = 1;
     const long long most_slabs = (a.space + 8 * step - 1) / (8 * step);
     if (slabs > most_slabs) slabs = most_slabs;

@@ -264,49 +264,35 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
     return r;
 }
 
-// V neighbouring channels in registers, two to a packed pair (V = 1: the upper half idles)
+// V neighbouring channels in registers
 template <int V>
 struct Vec {
-    static constexpr int N = (V + 1) / 2;
-    f32x2 p[N];
-    __device__ __forceinline__ float get(int i) const
-    {
-        const float2 v = halves(p[i / 2]);
-        return i & 1 ? v.y : v.x;
-    }
+    float f[V];
+    __device__ __forceinline__ float get(int i) const { return f[i]; }
 };
 template <int V, typename F>
-__device__ __forceinline__ Vec<V> each(F f)                    // f(i): pair i
+__device__ __forceinline__ Vec<V> each(F f)                    // f(i): channel i
 {
     Vec<V> r;
 #pragma unroll
-    for (int i = 0; i < Vec<V>::N; ++i) r.p[i] = f(i);
+    for (int i = 0; i < V; ++i) r.f[i] = f(i);
     return r;
 }
 template <int V>
-__device__ __forceinline__ Vec<V> splat(float v) { return each<V>([&](int) { return pair(v, v); }); }
+__device__ __forceinline__ Vec<V> splat(float v) { return each<V>([&](int) { return v; }); }
 template <int V>
-__device__ __forceinline__ Vec<V> fma2(const Vec<V> &a, const Vec<V> &b, const Vec<V> &c)
+__device__ __forceinline__ Vec<V> vfma(const Vec<V> &a, const Vec<V> &b, const Vec<V> &c)
 {
-    return each<V>([&](int i) { return fma2(a.p[i], b.p[i], c.p[i]); });
+    return each<V>([&](int i) { return fmaf(a.f[i], b.f[i], c.f[i]); });
 }
 template <int V>
-__device__ __forceinline__ Vec<V> mul2(const Vec<V> &a, const Vec<V> &b) { return each<V>([&](int i) { return mul2(a.p[i], b.p[i]); }); }
+__device__ __forceinline__ Vec<V> vmul(const Vec<V> &a, const Vec<V> &b) { return each<V>([&](int i) { return a.f[i] * b.f[i]; }); }
 template <int V>
-__device__ __forceinline__ Vec<V> add2(const Vec<V> &a, const Vec<V> &b) { return each<V>([&](int i) { return add2(a.p[i], b.p[i]); }); }
+__device__ __forceinline__ Vec<V> vadd(const Vec<V> &a, const Vec<V> &b) { return each<V>([&](int i) { return a.f[i] + b.f[i]; }); }
 template <typename T, int V>
-__device__ __forceinline__ Vec<V> widen(const Pack<T, V> &v)
-{
-    return each<V>([&](int i) { return pair(v.get(2 * i), 2 * i + 1 < V ? v.get(2 * i + 1) : 0.0f); });
-}
+__device__ __forceinline__ Vec<V> widen(const Pack<T, V> &v) { return each<V>([&](int i) { return v.get(i); }); }
 template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> narrow(const Vec<V> &v)
-{
-    float f[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = v.get(i);
-    return pack<T, V>(f);
-}
+__device__ __forceinline__ Pack<T, V> narrow(const Vec<V> &v) { return pack<T, V>(v.f); }
 // V neighbouring parameters (fp32 or T), one access where `wide`; `otherwise` where there are none
 template <typename T, int V>
 __device__ __forceinline__ Vec<V> load_params(const void *p, long long at, bool f32, bool wide, float otherwise)
@@ -315,11 +301,24 @@ __device__ __forceinline__ Vec<V> load_params(const void *p, long long at, bool 
     if constexpr (V > 1 && V * sizeof(float) <= 16) {
         if (wide) return f32 ? widen(load_pack<float, V>(static_cast<const float *>(p) + at)) : widen(load_pack<T, V>(static_cast<const T *>(p) + at));
     }
-    float f[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = f32 ? static_cast<const float *>(p)[at + i] : to_f32(static_cast<const T *>(p)[at + i]);
-    return each<V>([&](int i) { return pair(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.0f); });
+    return each<V>([&](int i) { return f32 ? static_cast<const float *>(p)[at + i] : to_f32(static_cast<const T *>(p)[at + i]); });
 }
+
+// ---- asynchronous copies into a thread's own part of shared memory ---------------------------------------------
+// A streaming kernel needs about 45 KB of loads in flight per SM to run at the memory's rate; as registers of the threads
+// that wait for them they would cost the occupancy that hides everything else.  Each thread copies what it will read
+// itself, so no barrier is involved: it waits for its own copies only.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *to, const void *from)
+{
+    static_assert(BYTES == 4 || BYTES == 8 || BYTES == 16, "sizes of an asynchronous copy");
+    const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>                      // at most LEFT of this thread's groups are still on their way
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // ---- elementary functions -------------------------------------------------------------------------------------
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.92596299e-8f;   // log2(e) as two floats
@@ -383,20 +382,14 @@ __device__ __forceinline__ f32x2 sigmoid2(f32x2 v)
     return pair(rcp_fast(w.x), rcp_fast(w.y));
 }
 __device__ __forceinline__ f32x2 silu2(f32x2 v) { return mul2(v, sigmoid2(v)); }
-template <int V>
-__device__ __forceinline__ Vec<V> silu2(const Vec<V> &v) { return each<V>([&](int i) { return silu2(v.p[i]); }); }
-// d silu / dv = s (1 + v (1 - s)), s = 1 / (1 + exp(-v))
-template <int V>
-__device__ __forceinline__ Vec<V> silu_slope2(const Vec<V> &v)
-{
-    return each<V>([&](int i) {
-        const f32x2 s = sigmoid2(v.p[i]);
-        return mul2(s, fma2(v.p[i], fma2(s, pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), pair(1.0f, 1.0f)));
-    });
-}
 __device__ __forceinline__ float sigmoid(float v) { return rcp_fast(1.0f + exp2_fast(-kLog2e * v)); }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
 __device__ __forceinline__ float silu_slope(float v, float sig) { return sig * fmaf(v, 1.0f - sig, 1.0f); }
+
+template <int V>
+__device__ __forceinline__ Vec<V> vsilu(const Vec<V> &v) { return each<V>([&](int i) { return silu(v.f[i]); }); }
+template <int V>
+__device__ __forceinline__ Vec<V> vsilu_slope(const Vec<V> &v) { return each<V>([&](int i) { return silu_slope(v.f[i], sigmoid(v.f[i])); }); }
 
 // ---- host side ------------------------------------------------------------------------------------------------
 void count_launches(int n);                  // sysconv_api.cu
