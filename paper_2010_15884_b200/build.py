@@ -3,7 +3,8 @@
 ``python -m paper_2010_15884_b200.build`` compiles every ``csrc/*.cu`` to an
 object (in parallel, only when the source or one of the headers it includes,
 as recorded by the compiler in a dependency file, is newer than the object)
-and links them into ``paper_2010_15884_b200/libsysconv.so``.  No GPU is needed.
+and links them into ``paper_2010_15884_b200/libsysconv.so``.  No GPU is needed.  ``_sequence.so``, which hands tensors to the
+library's sequence operators without a Python layer in between, is built with the host compiler beside it.
 """
 import concurrent.futures
 import glob
@@ -15,6 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libsysconv.so")
+EXT_SOURCE = os.path.join(CSRC, "sequence_ext.cpp")
+EXT_PATH = os.path.join(HERE, "_sequence.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -69,8 +72,31 @@ def _compile(src, obj, verbose):
     return res.stderr
 
 
+def _extension(force):
+    """Build _sequence.so if it is older than its source or the header; needs PyTorch's headers."""
+    header = os.path.join(HERE, "..", "include", "sysconv_sequence.h")
+    newest = max(os.path.getmtime(p) for p in (EXT_SOURCE, header, os.path.abspath(__file__)))
+    if not force and os.path.exists(EXT_PATH) and os.path.getmtime(EXT_PATH) > newest:
+        return
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = EXT_PATH + ".tmp.%d" % os.getpid()
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.sep in _nvcc() else "/usr/local/cuda"
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    cmd += ["-I" + p for p in cpp_extension.include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]]
+    cmd += [EXT_SOURCE, "-o", tmp, "-L" + HERE, "-l:libsysconv.so", "-Wl,-rpath,$ORIGIN", "-L" + libs, "-lc10", "-lc10_cuda",
+            "-ltorch_cpu", "-ltorch", "-ltorch_python"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed for %s:\n%s\n%s" % (EXT_SOURCE, res.stdout, res.stderr))
+    os.replace(tmp, EXT_PATH)
+
+
 def build(force=False, verbose=False, jobs=None):
-    """Compile and link the CUDA library; returns the path of the shared object."""
+    """Compile and link the CUDA library and the module that calls it; returns the path of the library."""
     os.makedirs(OBJ_DIR, exist_ok=True)
     sources = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
     if not sources:
@@ -97,6 +123,7 @@ def build(force=False, verbose=False, jobs=None):
         if res.returncode != 0:
             raise RuntimeError("link failed:\n%s\n%s" % (res.stdout, res.stderr))
         os.replace(tmp, LIB_PATH)
+    _extension(force)
     return LIB_PATH
 
 

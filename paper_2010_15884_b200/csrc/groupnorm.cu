@@ -7,8 +7,8 @@
 // Bound: memory; 4 bytes per 16-bit element forward, 6 backward.  Sums run over x - K with K the group's first element, so
 // that a mean far from zero costs no digits.  V neighbouring channels (all of one group) move as one access.
 //
-//  * Small groups (a warp's registers hold one): a warp reads its group once, reduces by shuffles and writes; it goes on
-//    to the same group of further batch entries with w and b in registers and the next entry's loads in flight.
+//  * No space (tokens): a block's threads hold whole rows of channels in registers; read once, written once.
+//  * Little space (a warp's registers hold a group), forward: a warp per group; read once, written once.
 //  * Everything else: partial sums per slab of rows, a small kernel that joins the slabs in a fixed order, and a second
 //    pass.  The second pass walks the slabs from the last to the first: the end of what the first pass read is still
 //    in the 126 MB L2.
@@ -51,9 +51,253 @@ __device__ __forceinline__ float2 warp_sum(float2 v)
     return v;
 }
 
-// ---- a warp per group ------------------------------------------------------------------------------------------------
+// ---- tokens: no space to reduce over ------------------------------------------------------------------------------------
+// A block takes rows of channels: min(256, C/V) threads to a row, Q vectors to a thread, as many rows at once as 256 threads
+// hold, and goes on to later rows; their vectors arrive by asynchronous copies, DEPTH - 1 rows ahead.  A group is L = cg/V
+// neighbouring vectors.  Its sums are added by exchanges inside runs of P vectors, P the largest power of two that divides L
+// (at most 32); if L > P the L/P parts meet in shared memory, in two buffers, so that one barrier per row is enough.  A warp's
+// vectors are neighbours (32 Q of them); where a group holds them all, a thread joins its own Q first (`fold`).
 
-template <typename T, int V, int R, bool BACK>
+struct TokenArgs {
+    NormArgs n;
+    int threads, rows, parts, run;       // threads per row, rows per block, L/P (fold: L/(32 Q)), P
+    bool fold;
+};
+
+template <typename T, int V, int Q, bool BACK>
+struct TokenRing {
+    static constexpr int BYTES = V * static_cast<int>(sizeof(T)), STREAMS = BACK ? 2 : 1;
+    static constexpr bool ASYNC = BYTES >= 4;
+    static constexpr int FIT = 32 * 1024 / (kNormThreads * BYTES * Q * STREAMS);
+    static constexpr int DEPTH = ASYNC ? (FIT > 8 ? 8 : (FIT < 2 ? 2 : FIT)) : 1;
+    static constexpr size_t bytes() { return ASYNC ? static_cast<size_t>(DEPTH) * STREAMS * Q * kNormThreads * BYTES : 16; }
+};
+// registers are what limits the blocks per SM
+template <int V, int Q, bool BACK> struct TokenBlocks { static constexpr int value = BACK ? (V * Q <= 8 ? 3 : (V * Q <= 16 ? 2 : 1)) : (V * Q <= 16 ? 3 : 2); };
+
+template <typename T, int V, int Q, bool BACK>
+__global__ void __launch_bounds__(kNormThreads, (TokenBlocks<V, Q, BACK>::value)) norm_token_kernel(TokenArgs k)
+{
+    using G = TokenRing<T, V, Q, BACK>;
+    constexpr int DEPTH = G::DEPTH, BYTES = G::BYTES;
+    extern __shared__ __align__(16) char norm_smem[];
+    __shared__ float2 part[2][Q * kNormThreads];
+    const NormArgs &a = k.n;
+    dependent_launch_enter();
+    const int ry = threadIdx.x / k.threads, tx = threadIdx.x - ry * k.threads;
+    const bool live = ry < k.rows;
+    const int vectors = a.channels / V;
+    const float inv = 1.0f / static_cast<float>(a.cg);
+    bool ok[Q], lead[Q];                                                 // lead: the group's first vector
+    int c[Q], group[Q], entry[Q];                                        // entry: of the group's first run, in `part`
+    Vec<V> w[Q], bias[Q], db[BACK ? Q : 1], dw[BACK ? Q : 1];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int cv = (tx / 32 * Q + q) * 32 + tx % 32;                 // (Q > 1: 256 threads to a row)
+        ok[q] = live && cv < vectors;
+        c[q] = ok[q] ? cv * V : 0;
+        group[q] = c[q] / a.cg;
+        lead[q] = ok[q] && c[q] == group[q] * a.cg;
+        entry[q] = group[q] * k.parts * (k.fold ? 1 : k.run);
+        w[q] = load_params<float, V>(a.w, c[q], true, false, 1.0f);
+        bias[q] = load_params<float, V>(a.b, c[q], true, false, 0.0f);
+        if (BACK) db[q] = dw[q] = splat<V>(0.0f);
+    }
+    const long long step = static_cast<long long>(gridDim.x) * k.rows;
+    const long long b0 = static_cast<long long>(blockIdx.x) * k.rows + ry;
+    const long long rounds = (a.batch - static_cast<long long>(blockIdx.x) * k.rows + step - 1) / step;    // the same for the whole block
+    const Tokens &out_t = BACK ? a.dx : a.y;
+    const T *px = static_cast<const T *>(a.x.ptr) + b0 * a.x.bstride;
+    const T *pd = BACK ? static_cast<const T *>(a.dy.ptr) + b0 * a.dy.bstride : nullptr;
+    T *po = static_cast<T *>(out_t.ptr) + b0 * out_t.bstride;
+    long long ahead = b0;                                                // the row px and pd point to
+    auto slot = [&](int s, int stream, int q) { return norm_smem + (((s * G::STREAMS + stream) * Q + q) * kNormThreads + threadIdx.x) * BYTES; };
+    auto fill = [&](int s) {
+        if constexpr (G::ASYNC) {
+            if (ahead < a.batch)
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (ok[q]) {
+                        copy_async<BYTES>(slot(s, 0, q), px + c[q]);
+                        if (BACK) copy_async<BYTES>(slot(s, 1, q), pd + c[q]);
+                    }
+            ahead += step;
+            px += step * a.x.bstride;
+            if (BACK) pd += step * a.dy.bstride;
+        }
+        copy_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < DEPTH - 1; ++s) fill(s);
+    int s = 0;
+    long long b = b0;
+    for (long long i = 0; i < rounds; ++i, b += step, po += step * out_t.bstride) {
+        const bool here = b < a.batch;
+        Vec<V> x[Q], e[BACK ? Q : 1];
+        if constexpr (G::ASYNC) {
+            copy_wait<DEPTH - 2>();
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                x[q] = widen(load_pack<T, V>(reinterpret_cast<const T *>(slot(s, 0, q))));
+                if (BACK) e[q] = widen(load_pack<T, V>(reinterpret_cast<const T *>(slot(s, 1, q))));
+            }
+            fill(s == 0 ? DEPTH - 1 : s - 1);
+            s = s + 1 == DEPTH ? 0 : s + 1;
+        } else {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const bool get = ok[q] && here;
+                x[q] = get ? widen(load_pack<T, V>(px + c[q])) : splat<V>(0.0f);
+                if (BACK) e[q] = get ? widen(load_pack<T, V>(pd + c[q])) : splat<V>(0.0f);
+            }
+            px += step * a.x.bstride;
+            if (BACK) pd += step * a.dy.bstride;
+        }
+        // Forward: mean and sum of squares about it, of V channels, then joined in equal shares: (m, s) and (m', s') of n
+        // channels each give (m + m') / 2 and s + s' + (m - m')^2 n / 2, which costs no digits wherever the mean lies.
+        // Backward: the sums of p and p xhat.
+        float2 sum[Q];
+        float rstd[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            sum[q] = make_float2(0.0f, 0.0f);
+            rstd[q] = 0.0f;
+            if (BACK) {
+                if (ok[q] && here) {
+                    const long long bg = b * a.groups + group[q];
+                    const float mean = a.mean[bg];
+                    rstd[q] = a.rstd[bg];
+                    x[q] = vmul(vadd(x[q], splat<V>(-mean)), splat<V>(rstd[q]));
+                    if (a.silu) e[q] = vmul(e[q], vsilu_slope(vfma(x[q], w[q], bias[q])));
+                    db[q] = vadd(db[q], e[q]);
+                    dw[q] = vfma(e[q], x[q], dw[q]);
+                    e[q] = vmul(e[q], w[q]);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        sum[q].x += e[q].get(j);
+                        sum[q].y = fmaf(e[q].get(j), x[q].get(j), sum[q].y);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[q].x += x[q].get(j);
+                sum[q].x *= 1.0f / V;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float d = x[q].get(j) - sum[q].x;
+                    sum[q].y = fmaf(d, d, sum[q].y);
+                }
+            }
+        }
+        auto exchange = [&](float2 &v, int level, float n) {             // runs of 2^level of n channels each: pairs of them
+            const float ox = __shfl_xor_sync(kFullMask, v.x, 1 << level), oy = __shfl_xor_sync(kFullMask, v.y, 1 << level);
+            if (BACK) {
+                v.x += ox;
+                v.y += oy;
+            } else {
+                const float d = v.x - ox;
+                v.y = fmaf(d * d, 0.5f * n, v.y + oy);
+                v.x = 0.5f * (v.x + ox);
+            }
+        };
+        auto join = [&](const float2 *buffer, int at, int step, int parts, float n) {      // equal shares from shared memory
+            float2 v = make_float2(0.0f, 0.0f);
+            for (int j = 0; j < parts; ++j) {
+                v.x += buffer[at + j * step].x;
+                v.y += buffer[at + j * step].y;
+            }
+            if (!BACK) {
+                v.x /= static_cast<float>(parts);
+                for (int j = 0; j < parts; ++j) {
+                    const float d = buffer[at + j * step].x - v.x;
+                    v.y = fmaf(d * d, n, v.y);
+                }
+            }
+            return v;
+        };
+        float2 *buffer = &part[i & 1][0];
+        if (k.fold) {
+            float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                v.x += sum[q].x;
+                v.y += sum[q].y;
+            }
+            if (!BACK) {
+                v.x *= 1.0f / Q;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) v.y = fmaf((sum[q].x - v.x) * (sum[q].x - v.x), V, v.y);
+            }
+#pragma unroll
+            for (int level = 0; level < 5; ++level) exchange(v, level, Q * V << level);
+            if (k.parts > 1) {
+                if ((threadIdx.x & 31) == 0) buffer[threadIdx.x >> 5] = v;
+                __syncthreads();
+                v = join(buffer, entry[0], 1, k.parts, 32 * Q * V);
+            }
+#pragma unroll
+            for (int q = 0; q < Q; ++q) sum[q] = v;
+        } else {
+#pragma unroll
+            for (int level = 0; level < 5; ++level)
+                if (1 << level < k.run)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) exchange(sum[q], level, V << level);
+            if (k.parts > 1) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (ok[q]) buffer[ry * k.threads + c[q] / V] = sum[q];
+                __syncthreads();
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (ok[q]) sum[q] = join(buffer, ry * k.threads + entry[q], k.run, k.parts, static_cast<float>(V * k.run));
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (!ok[q] || !here) continue;
+            if (BACK) {
+                store_pack(po + c[q], narrow<T, V>(vmul(splat<V>(rstd[q]), vadd(vfma(x[q], splat<V>(-sum[q].y * inv), splat<V>(-sum[q].x * inv)), e[q]))));
+            } else {
+                const float mean = sum[q].x;
+                rstd[q] = rsqrtf(fmaf(sum[q].y, inv, a.eps));
+                if (lead[q]) {
+                    if (a.mean) a.mean[b * a.groups + group[q]] = mean;
+                    if (a.rstd) a.rstd[b * a.groups + group[q]] = rstd[q];
+                }
+                Vec<V> v = vfma(vadd(x[q], splat<V>(-mean)), vmul(w[q], splat<V>(rstd[q])), bias[q]);
+                if (a.silu) v = vsilu(v);
+                store_pack(po + c[q], narrow<T, V>(v));
+            }
+        }
+    }
+    if (!BACK || a.pq == nullptr) return;
+    // dw and db of the block's rows, one row of pq: the first row of threads adds the others'
+    copy_wait<0>();
+    float *to = a.pq + static_cast<long long>(blockIdx.x) * 2 * a.channels;
+    float *sums = reinterpret_cast<float *>(part);                       // [threads]
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int j = 0; j < 2 * V; ++j) {
+            const float v = j < V ? db[q].get(j % V) : dw[q].get(j % V);
+            float all = v;
+            if (k.rows > 1) {
+                __syncthreads();
+                sums[threadIdx.x] = v;
+                __syncthreads();
+                if (ry == 0)
+                    for (int r = 1; r < k.rows; ++r) all += sums[r * k.threads + tx];
+            }
+            if (ok[q] && ry == 0) to[(j / V) * a.channels + c[q] + j % V] = all;
+        }
+}
+
+// ---- a warp per group: a little space ---------------------------------------------------------------------------------
+// A warp reads its group once, reduces by shuffles and writes; it goes on to the same group of further batch entries with
+// w and b in registers and the next entry's loads in flight.
+
+template <typename T, int V, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
 {
     dependent_launch_enter();
@@ -66,113 +310,57 @@ __global__ void __launch_bounds__(kNormThreads) norm_warp_kernel(NormArgs a)
     const int count = static_cast<int>(a.space) * per_row;               // vectors of the group
     const float inv = 1.0f / static_cast<float>(static_cast<long long>(count) * V);
     // offsets of this lane's vectors within a batch entry; those that do not exist repeat the first one and do not count
-    long long at_x[R], at_y[R], at_d[BACK ? R : 1];
-    int at_c[R];
+    long long at_x[R], at_y[R];
     bool ok[R];
-    Vec<V> wv[R], bv[R], db[BACK ? R : 1], dw[BACK ? R : 1];
-    const Tokens &out_t = BACK ? a.dx : a.y;
+    Vec<V> wv[R], bv[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         ok[i] = lane + 32 * i < count;
-        const int q = ok[i] ? lane + 32 * i : 0, s = q / per_row;
-        at_c[i] = g * a.cg + (q - s * per_row) * V;
-        at_x[i] = s * a.x.tstride + at_c[i];
-        at_y[i] = s * out_t.tstride + at_c[i];
-        if (BACK) at_d[i] = s * a.dy.tstride + at_c[i];
-        wv[i] = load_params<float, V>(a.w, at_c[i], true, false, 1.0f);
-        bv[i] = load_params<float, V>(a.b, at_c[i], true, false, 0.0f);
-        if (BACK) db[i] = dw[i] = splat<V>(0.0f);
+        const int q = ok[i] ? lane + 32 * i : 0, s = q / per_row, c = g * a.cg + (q - s * per_row) * V;
+        at_x[i] = s * a.x.tstride + c;
+        at_y[i] = s * a.y.tstride + c;
+        wv[i] = load_params<float, V>(a.w, c, true, false, 1.0f);
+        bv[i] = load_params<float, V>(a.b, c, true, false, 0.0f);
     }
-    Pack<T, V> raw[R], rdy[BACK ? R : 1];
+    Pack<T, V> raw[R];
     const T *px = static_cast<const T *>(a.x.ptr) + row * a.x.bstride;
-    const T *pd = BACK ? static_cast<const T *>(a.dy.ptr) + row * a.dy.bstride : nullptr;
-    T *po = static_cast<T *>(out_t.ptr) + row * out_t.bstride;
+    T *po = static_cast<T *>(a.y.ptr) + row * a.y.bstride;
     auto fetch = [&]() {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            raw[i] = load_pack<T, V>(px + at_x[i]);
-            if (BACK) rdy[i] = load_pack<T, V>(pd + at_d[i]);
-        }
+        for (int i = 0; i < R; ++i) raw[i] = load_pack<T, V>(px + at_x[i]);
         px += a.entry_step * a.x.bstride;
-        if (BACK) pd += a.entry_step * a.dy.bstride;
     };
     if (row < a.batch) fetch();
     for (long long b = row; b < a.batch; b += a.entry_step) {
-        Vec<V> x[R], e[BACK ? R : 1];
+        Vec<V> x[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            x[i] = widen(raw[i]);
-            if (BACK) e[i] = widen(rdy[i]);
-        }
+        for (int i = 0; i < R; ++i) x[i] = widen(raw[i]);
         if (b + a.entry_step < a.batch) fetch();
-        if (!BACK) {
-            const float shift = __shfl_sync(kFullMask, x[0].get(0), 0);
-            Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const Vec<V> v = vadd(x[i], splat<V>(ok[i] ? -shift : -x[i].get(0)));
-                if (ok[i]) {
-                    s1 = vadd(s1, v);
-                    s2 = vfma(v, v, s2);
-                }
-            }
-            float2 s = make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                s.x += s1.get(j);
-                s.y += s2.get(j);
-            }
-            s = warp_sum(s);
-            const float off = s.x * inv, mean = shift + off;
-            const float rstd = rsqrtf(fmaxf(fmaf(-off, off, s.y * inv), 0.0f) + a.eps);
-            if (lane == 0) {
-                if (a.mean) a.mean[b * a.groups + g] = mean;
-                if (a.rstd) a.rstd[b * a.groups + g] = rstd;
-            }
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                Vec<V> v = vfma(vadd(x[i], splat<V>(-mean)), vmul(wv[i], splat<V>(rstd)), bv[i]);
-                if (a.silu) v = vsilu(v);
-                if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(v));
-            }
-        } else {
-            const float mean = a.mean[b * a.groups + g], rstd = a.rstd[b * a.groups + g];
-            Vec<V> s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                x[i] = vmul(vadd(x[i], splat<V>(-mean)), splat<V>(rstd));
-                if (a.silu) e[i] = vmul(e[i], vsilu_slope(vfma(x[i], wv[i], bv[i])));
-                if (ok[i]) {
-                    db[i] = vadd(db[i], e[i]);
-                    dw[i] = vfma(e[i], x[i], dw[i]);
-                    e[i] = vmul(e[i], wv[i]);
-                    s1 = vadd(s1, e[i]);
-                    s2 = vfma(e[i], x[i], s2);
-                }
-            }
-            float2 s = make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                s.x += s1.get(j);
-                s.y += s2.get(j);
-            }
-            s = warp_sum(s);
-            const Vec<V> m1 = splat<V>(-s.x * inv), m2 = splat<V>(-s.y * inv);
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(vmul(splat<V>(rstd), vadd(vfma(x[i], m2, m1), e[i]))));
-        }
-        po += a.entry_step * out_t.bstride;
-    }
-    if (BACK && a.pq != nullptr) {                                       // space is 1 here: a channel belongs to one lane
+        const float shift = __shfl_sync(kFullMask, x[0].get(0), 0);
+        float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < R; ++i)
             if (ok[i])
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    a.pq[row * 2 * a.channels + at_c[i] + j] = db[i].get(j);
-                    a.pq[(row * 2 + 1) * a.channels + at_c[i] + j] = dw[i].get(j);
+                    const float v = x[i].get(j) - shift;
+                    s.x += v;
+                    s.y = fmaf(v, v, s.y);
                 }
+        s = warp_sum(s);
+        const float off = s.x * inv, mean = shift + off;
+        const float rstd = rsqrtf(fmaxf(fmaf(-off, off, s.y * inv), 0.0f) + a.eps);
+        if (lane == 0) {
+            if (a.mean) a.mean[b * a.groups + g] = mean;
+            if (a.rstd) a.rstd[b * a.groups + g] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            Vec<V> v = vfma(vadd(x[i], splat<V>(-mean)), vmul(wv[i], splat<V>(rstd)), bv[i]);
+            if (a.silu) v = vsilu(v);
+            if (ok[i]) store_pack(po + at_y[i], narrow<T, V>(v));
+        }
+        po += a.entry_step * a.y.bstride;
     }
 }
 
@@ -241,25 +429,28 @@ __device__ __forceinline__ void walk_rows(const SlabPlace &p, char *room, const 
             }
             copy_commit();
         }
-        int slot = 0, ahead = DEPTH - 1;
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
+        auto row = [&](int slot, bool more) {                            // uses `slot`, fills the one before it
             copy_wait<DEPTH - 2>();
             const char *at = own + slot * SLOT;
             const Pack<T, V> a = load_pack<T, V>(reinterpret_cast<const T *>(at));
             Pack<T, V> b = a;
             if (TWO) b = load_pack<T, V>(reinterpret_cast<const T *>(at + PITCH));
-            if (i + DEPTH - 1 < n) {
-                copy_async<BYTES>(own + ahead * SLOT, nx);
-                if (TWO) copy_async<BYTES>(own + ahead * SLOT + PITCH, ny);
+            if (more) {
+                char *to = own + (slot == 0 ? DEPTH - 1 : slot - 1) * SLOT;
+                copy_async<BYTES>(to, nx);
+                if (TWO) copy_async<BYTES>(to + PITCH, ny);
                 nx += sx;
                 if (TWO) ny += sy;
             }
             copy_commit();
-            slot = slot + 1 == DEPTH ? 0 : slot + 1;
-            ahead = ahead + 1 == DEPTH ? 0 : ahead + 1;
             f(widen(a), widen(b));
+        };
+        int i = 0;
+        for (; i + 2 * DEPTH - 1 <= n; i += DEPTH) {                     // whole rounds of the ring: slots known at compile time
+#pragma unroll
+            for (int s = 0; s < DEPTH; ++s) row(s, true);
         }
+        for (int s = 0; i < n; ++i, s = s + 1 == DEPTH ? 0 : s + 1) row(s, i + DEPTH - 1 < n);
         copy_wait<0>();
     }
 }
@@ -567,7 +758,10 @@ __global__ void __launch_bounds__(1024) norm_param_kernel(const float *pq, long 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 struct NormPlan {
-    int v, r;                    // channels per access, vectors per lane (warp form; 0: slabs)
+    int v;                       // channels per access
+    int q;                       // token form: vectors per thread (0: another form)
+    int threads, rows, run, blocks;
+    int r;                       // warp form: vectors per lane (0: slabs)
     int tile, tiles, rows_per_slab, slabs, entry_step;
     long long part_floats, pq_floats, sum_floats, stat_floats;
 };
@@ -583,18 +777,37 @@ NormPlan norm_plan(const sysgroupnorm_args &a, bool back)
         return rows_aligned(a.x, false, esz, bytes) && (back ? rows_aligned(a.dy, false, esz, bytes) && rows_aligned(a.dx, false, esz, bytes)
                                                              : rows_aligned(a.y, false, esz, bytes));
     };
-    // a warp per group: its vectors lie inside the group
+    // tokens, and a warp per group: vectors lie inside the group
     p.v = widest;
     while (p.v > 1 && (cg % p.v != 0 || !aligned(p.v))) p.v /= 2;
-    const long long vectors = a.space * (cg / p.v);
-    const int most = back ? 2 : 4;                                       // vectors per lane
-    if (vectors <= 32 * most && (!back || a.space == 1)) {
+    const long long row = a.channels / p.v, per_group = cg / p.v;
+    // a group of 125 vectors, say, falls into 125 runs of one: the token form then spends its time joining them (8191 rows of
+    // three groups of 1000 channels 204 us), the warp form does not care
+    int odd_part = static_cast<int>(per_group);
+    while (odd_part % 2 == 0) odd_part /= 2;
+    const bool joins = odd_part > 16 && !back && per_group <= 32 * 4;
+    if (a.space == 1 && !joins && row * p.v <= kNormThreads * 32LL) {
+        const int channels = p.v * ceil_div(row, kNormThreads);          // a thread's
+        p.q = ceil_div(row, kNormThreads);
+        if (p.q > 4) p.q = 8;
+        else if (p.q == 3) p.q = 4;
+        p.threads = row < kNormThreads ? static_cast<int>(row) : kNormThreads;
+        p.rows = kNormThreads / p.threads;
+        p.run = 1;
+        while (p.run < 32 && per_group % (2 * p.run) == 0 && p.threads % (2 * p.run) == 0) p.run *= 2;
+        const int resident = back ? (channels <= 8 ? 3 : (channels <= 16 ? 2 : 1)) : (channels <= 16 ? 3 : 2);
+        const long long blocks = (a.batch + p.rows - 1) / p.rows;
+        p.blocks = static_cast<int>(blocks < 148LL * resident ? blocks : 148LL * resident);
+        if (back) p.pq_floats = 2LL * p.blocks * a.channels;
+        return p;
+    }
+    const long long vectors = a.space * per_group;
+    if (!back && vectors <= 32 * 4) {
         p.r = vectors <= 32 ? 1 : (vectors <= 64 ? 2 : 4);
-        const long long warps = 148LL * (back ? 16 : 24);                // what the machine holds at once
+        const long long warps = 148LL * 16;                              // what the machine holds at once
         long long step = warps / a.groups;
         if (step < 1) step = 1;
         p.entry_step = static_cast<int>(step < a.batch ? step : a.batch);
-        if (back) p.pq_floats = 2LL * p.entry_step * a.channels;
         return p;
     }
     // slabs: a tile is all channels if a row of them has at most 256 vectors, else as many whole groups as do
@@ -670,16 +883,34 @@ cudaError_t with_width(int v, F f)
     }
 }
 
-template <typename T, int V, bool BACK>
+template <typename T, int V>
 cudaError_t launch_norm_warp(const NormArgs &k, const NormPlan &p, cudaStream_t s)
 {
     const dim3 grid(ceil_div(static_cast<long long>(p.entry_step) * k.groups, kNormThreads / 32)), block(kNormThreads);
     switch (p.r) {
-        case 1: return launch_kernel(norm_warp_kernel<T, V, 1, BACK>, grid, block, s, k);
-        case 2: return launch_kernel(norm_warp_kernel<T, V, 2, BACK>, grid, block, s, k);
-        default:
-            if constexpr (BACK) return kNoInstantiation;
-            else return launch_kernel(norm_warp_kernel<T, V, 4, BACK>, grid, block, s, k);
+        case 1: return launch_kernel(norm_warp_kernel<T, V, 1>, grid, block, s, k);
+        case 2: return launch_kernel(norm_warp_kernel<T, V, 2>, grid, block, s, k);
+        default: return launch_kernel(norm_warp_kernel<T, V, 4>, grid, block, s, k);
+    }
+}
+
+template <typename T, int V, bool BACK>
+cudaError_t launch_norm_tokens(const NormArgs &k, const NormPlan &p, cudaStream_t s)
+{
+    const int per_group = k.cg / V;
+    const bool fold = p.threads == kNormThreads && k.channels / V == kNormThreads * p.q && per_group % (32 * p.q) == 0;
+    TokenArgs a = {k, p.threads, p.rows, fold ? per_group / (32 * p.q) : per_group / p.run, p.run, fold};
+    auto go = [&](auto q) -> cudaError_t {
+        constexpr int Q = decltype(q)::value;
+        if constexpr (V * Q <= 32)
+            return launch_kernel_smem(norm_token_kernel<T, V, Q, BACK>, dim3(p.blocks), dim3(kNormThreads), TokenRing<T, V, Q, BACK>::bytes(), s, a);
+        else return kNoInstantiation;
+    };
+    switch (p.q) {
+        case 1: return go(Width<1>{});
+        case 2: return go(Width<2>{});
+        case 4: return go(Width<4>{});
+        default: return go(Width<8>{});
     }
 }
 
@@ -724,9 +955,9 @@ cudaError_t launch_groupnorm(const sysgroupnorm_args &a, cudaStream_t s, int *la
         using T = std::remove_pointer_t<decltype(tag)>;
         return with_width<T>(p.v, [&](auto width) -> cudaError_t {
             constexpr int V = decltype(width)::value;
-            if (p.r > 0) {
+            if (p.q > 0 || p.r > 0) {
                 *launches += 1;
-                return launch_norm_warp<T, V, false>(k, p, s);
+                return p.q > 0 ? launch_norm_tokens<T, V, false>(k, p, s) : launch_norm_warp<T, V>(k, p, s);
             }
             float *stats = k.part + p.part_floats;
             if (k.mean == nullptr) k.mean = stats;
@@ -753,9 +984,9 @@ cudaError_t launch_groupnorm_backward(const sysgroupnorm_args &a, cudaStream_t s
         using T = std::remove_pointer_t<decltype(tag)>;
         return with_width<T>(p.v, [&](auto width) -> cudaError_t {
             constexpr int V = decltype(width)::value;
-            if (p.r > 0) {
+            if (p.q > 0) {
                 *launches += 1;
-                return launch_norm_warp<T, V, true>(k, p, s);
+                return launch_norm_tokens<T, V, true>(k, p, s);
             }
             return by_entries(k, sizeof(T), [&](NormArgs q, long long b0) {
                 q.part = k.part + b0 * k.slabs * 2 * k.channels;
@@ -774,7 +1005,7 @@ cudaError_t launch_groupnorm_backward(const sysgroupnorm_args &a, cudaStream_t s
     });
     if (err != cudaSuccess || !params) return err;
     *launches += 1;
-    const long long rows = p.r > 0 ? p.entry_step : a.batch;
+    const long long rows = p.q > 0 ? p.blocks : a.batch;
     return launch_kernel(norm_param_kernel, dim3(ceil_div(a.channels, 32)), dim3(32, 32), s, k.pq, rows, k.channels,
                          static_cast<float *>(a.dweight), static_cast<float *>(a.dbias));
 }

@@ -190,11 +190,14 @@ struct SeqMap {
             return static_cast<int>(r < sequences ? r : sequences - 1);
         }
         int lo = 0, hi = sequences - 1;
-        while (lo < hi) {
+        while (hi - lo > 16) {
             const int mid = (lo + hi + 1) >> 1;
             if (first(mid) <= t) lo = mid; else hi = mid - 1;
         }
-        return lo;
+        int at = lo;                                   // the last few by loads that do not wait for each other
+#pragma unroll 4
+        for (int r = lo + 1; r <= hi; ++r) at = first(r) <= t ? r : at;
+        return at;
     }
 };
 

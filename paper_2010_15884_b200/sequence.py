@@ -23,6 +23,11 @@ import torch
 from . import binding
 from .binding import SysconvError
 
+try:
+    from . import _sequence                     # the same calls, marshalled in C++; None from it: the code here decides
+except ImportError:                             # (not built: every call takes the way through this file)
+    _sequence = None
+
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _ACTS = {None: 0, "none": 0, "silu": 1}
 
@@ -186,6 +191,10 @@ def conv1d_causal(x, weight, bias=None, activation=None, state=None, offsets=Non
     weight (channels, taps), taps <= 8; bias (channels); both float32 or of x's type.  state (sequences, taps-1, channels) of
     x's type: the inputs before the first token (zeros without it).  Returns y, or (y, final state) with return_state.
     """
+    if _sequence is not None and stream is None and out is None:
+        r = _sequence.conv(x, weight, bias, activation, state, offsets, return_state)
+        if r is not None:
+            return r
     if _elsewhere(x, stream):
         with _there(x, stream, "conv1d_causal"):
             return conv1d_causal(x, weight, bias, activation, state, offsets, return_state, out)
@@ -208,6 +217,10 @@ def conv1d_causal_backward(dy, x, weight, bias=None, activation=None, state=None
 
     dfinal: gradient with respect to the final state, if that was used.
     """
+    if _sequence is not None and stream is None:
+        r = _sequence.conv_backward(dy, x, weight, bias, activation, state, offsets, dfinal)
+        if r is not None:
+            return r
     if _elsewhere(x, stream):
         with _there(x, stream, "conv1d_causal_backward"):
             return conv1d_causal_backward(dy, x, weight, bias, activation, state, offsets, dfinal)
@@ -239,6 +252,10 @@ def conv1d_causal_step(x, state, weight, bias=None, activation=None, slots=None,
     slots (int32, one per row): the slot of each row; a slot outside the cache (-1, say) gives zeros and touches no
     state.  Without it row r uses slot r.  No two rows may name the same slot.
     """
+    if _sequence is not None and stream is None and out is None:
+        r = _sequence.conv_step(x, state, weight, bias, activation, slots)
+        if r is not None:
+            return r
     if _elsewhere(x, stream):
         with _there(x, stream, "conv1d_causal_step"):
             return conv1d_causal_step(x, state, weight, bias, activation, slots, out)
@@ -328,6 +345,10 @@ def state_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=Fals
     (sequences, channels, states): float32.  states <= 128.
     Returns y; with return_state also the final state, with save also what state_scan_backward needs, in this order.
     """
+    if _sequence is not None and stream is None and out is None:
+        r = _sequence.scan(u, delta, A, B, C, D, z, delta_bias, softplus, state, offsets, longest, return_state, save)
+        if r is not None:
+            return r
     if _elsewhere(u, stream):
         with _there(u, stream, "state_scan"):
             return state_scan(u, delta, A, B, C, D, z, delta_bias, softplus, state, offsets, longest, return_state, save, out)
@@ -359,6 +380,11 @@ def state_scan_backward(dy, u, delta, A, B, C, saved, D=None, z=None, delta_bias
     dfinal: gradient with respect to the final state, if that was used.  dz, dD, ddelta_bias are None where z, D, delta_bias
     are; dstate (the gradient with respect to the initial state) is computed on state_grad.
     """
+    if _sequence is not None and stream is None:
+        r = _sequence.scan_backward(u, delta, A, B, C, dy, saved, D, z, delta_bias, softplus, offsets, longest, dfinal,
+                                     state_grad)
+        if r is not None:
+            return ScanGrads(*r)
     if _elsewhere(u, stream):
         with _there(u, stream, "state_scan_backward"):
             return state_scan_backward(dy, u, delta, A, B, C, saved, D, z, delta_bias, softplus, offsets, longest, dfinal, state_grad)
@@ -392,6 +418,10 @@ def state_scan_backward(dy, u, delta, A, B, C, saved, D=None, z=None, delta_bias
 def state_scan_step(u, delta, A, B, C, state, D=None, z=None, delta_bias=None, softplus=False, slots=None, out=None, stream=None):
     """One token of each row: u, delta, z (rows, channels), B, C (rows[, groups], states); state (slots, channels, states),
     float32, is updated in place.  Slots as in conv1d_causal_step.  Returns y."""
+    if _sequence is not None and stream is None and out is None:
+        r = _sequence.scan_step(u, delta, A, B, C, state, D, z, delta_bias, softplus, slots)
+        if r is not None:
+            return r
     if _elsewhere(u, stream):
         with _there(u, stream, "state_scan_step"):
             return state_scan_step(u, delta, A, B, C, state, D, z, delta_bias, softplus, slots, out)
@@ -453,6 +483,10 @@ def groupnorm(x, groups, weight=None, bias=None, eps=1e-5, activation=None, retu
     """Group norm, channels last: x (batch, ..., channels) is normalised over everything between batch and channels and
     over the channels of each group; y = act((x - mean) * rstd * weight + bias).  weight, bias (channels), float32.
     Returns y, or (y, mean, rstd) with return_stats, which groupnorm_backward needs."""
+    if _sequence is not None and stream is None and out is None:
+        r = _sequence.norm(x, groups, weight, bias, eps, activation, return_stats)
+        if r is not None:
+            return r
     if _elsewhere(x, stream):
         with _there(x, stream, "groupnorm"):
             return groupnorm(x, groups, weight, bias, eps, activation, return_stats, out)
@@ -476,6 +510,10 @@ def groupnorm(x, groups, weight=None, bias=None, eps=1e-5, activation=None, retu
 
 def groupnorm_backward(dy, x, groups, mean, rstd, weight=None, bias=None, activation=None, stream=None):
     """Gradients of groupnorm: (dx, dweight, dbias), the last two None where weight or bias is None."""
+    if _sequence is not None and stream is None:
+        r = _sequence.norm_backward(dy, x, groups, mean, rstd, weight, bias, activation)
+        if r is not None:
+            return r
     if _elsewhere(x, stream):
         with _there(x, stream, "groupnorm_backward"):
             return groupnorm_backward(dy, x, groups, mean, rstd, weight, bias, activation)
