@@ -35,10 +35,12 @@ struct ScanBackArgs {
 template <int LN, int S>
 struct ScanBackShape {
     static constexpr int NP = LN * S;
-    static constexpr int NT = LN <= 8 ? 128 : (NP >= 128 ? 256 : 16 * LN);   // threads: 16 channels a block where they fit
+    // threads: 32 channels a block where they fit (its partial sums of dB and dC are read and written once more)
+    static constexpr int NT = LN <= 16 ? 256 : (NP >= 128 ? 256 : 512);
     static constexpr int CB = NT / LN;
     static constexpr int TB = kScanBlock;
-    static constexpr int U = LN < 16 ? LN : 16;
+    static constexpr int HB = 8;                                        // tokens whose states and decays are held in registers
+    static constexpr int U = LN < HB ? LN : HB;
     static constexpr int PP = TB * CB / NT > 0 ? TB * CB / NT : 1;
     static constexpr int VT = PP >= 4 ? 4 : PP;
     static constexpr int BE = TB * NP / NT > 0 ? TB * NP / NT : 1;
@@ -52,10 +54,10 @@ struct ScanBackShape {
 };
 
 template <typename T, int LN, int S, bool WIDE>
-__global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kernel(ScanBackArgs b)
+__global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackShape<LN, S>::NT)) scan_backward_kernel(ScanBackArgs b)
 {
     using G = ScanBackShape<LN, S>;
-    constexpr int NP = G::NP, NT = G::NT, CB = G::CB, TB = G::TB, U = G::U, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB;
+    constexpr int NP = G::NP, NT = G::NT, CB = G::CB, TB = G::TB, HB = G::HB, U = G::U, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB;
     constexpr int YP = G::YP, W = G::W, P2 = S / 2, NV = 2 * S, CW = 32 / LN;
     extern __shared__ __align__(16) float smem[];
     float4 *s_p = reinterpret_cast<float4 *>(smem);                      // [TB][CB] d, d u, dy'
@@ -193,100 +195,123 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT)) scan_backward_kern
                 }
             }
         }
-        f32x2 h[TB + 1][P2], dec[TB][P2];
+        f32x2 start[P2], dA_tile[P2];                                    // state before the tile
 #pragma unroll
-        for (int i = 0; i < P2; ++i) h[0][i] = pair(rh[2 * i], rh[2 * i + 1]);
+        for (int i = 0; i < P2; ++i) {
+            start[i] = pair(rh[2 * i], rh[2 * i + 1]);
+            dA_tile[i] = pair(0.0f, 0.0f);
+        }
         __syncthreads();
         if (tile > 0) fetch(t0 - TB);
 
-        // forwards: states and decays of the tile, y
+        // one token forwards: its decay, and the state after it
+        auto advance = [&](int t, const f32x2 (&from)[P2], f32x2 (&decay)[P2], f32x2 (&to)[P2]) {
+            const float2 d = *reinterpret_cast<const float2 *>(&s_p[t * CB + cl]);
 #pragma unroll
-        for (int tu = 0; tu < TB; tu += U) {
-            float sums[U];
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int t = tu + k;
-                const float2 d = *reinterpret_cast<const float2 *>(&s_p[t * CB + cl]);
-                f32x2 acc;
-#pragma unroll
-                for (int i = 0; i < P2; ++i) {
-                    const float2 bv = *reinterpret_cast<const float2 *>(&s_b[t * NP + ln * S + 2 * i]);
-                    const float2 cv = *reinterpret_cast<const float2 *>(&s_c[t * NP + ln * S + 2 * i]);
-                    const float2 x = halves(mul2(A2[i], pair(d.x, d.x)));
-                    dec[t][i] = pair(exp2_fast(x.x), exp2_fast(x.y));
-                    h[t + 1][i] = fma2(dec[t][i], h[t][i], mul2(pair(bv.x, bv.y), pair(d.y, d.y)));
-                    acc = i == 0 ? mul2(h[t + 1][i], pair(cv.x, cv.y)) : fma2(h[t + 1][i], pair(cv.x, cv.y), acc);
-                }
-                const float2 v = halves(acc);
-                sums[k] = v.x + v.y;
+            for (int i = 0; i < P2; ++i) {
+                const float2 bv = *reinterpret_cast<const float2 *>(&s_b[t * NP + ln * S + 2 * i]);
+                const float2 x = halves(mul2(A2[i], pair(d.x, d.x)));
+                decay[i] = pair(exp2_fast(x.x), exp2_fast(x.y));
+                to[i] = fma2(decay[i], from[i], mul2(pair(bv.x, bv.y), pair(d.y, d.y)));
             }
-            if (gate) {
-                const float v = sum_transposed<U, LN>(sums, lane);
-                if (LN <= U || ln < U) s_y[(tu + ln % U) * YP + cl] = v;
-            }
+        };
+        // The second half of the tile first, from a state that is reached without keeping the way to it: holding all 16 tokens'
+        // states and decays would take twice the registers and halve the warps per scheduler.
+        f32x2 middle[P2];
+#pragma unroll
+        for (int i = 0; i < P2; ++i) middle[i] = start[i];
+#pragma unroll
+        for (int t = 0; t < TB - HB; ++t) {
+            f32x2 unused[P2];
+            advance(t, middle, unused, middle);
         }
-        // backwards
-        f32x2 dA_tile[P2];
+#pragma unroll 1
+        for (int base = TB - HB; base >= 0; base -= HB) {
+            f32x2 h[HB + 1][P2], dec[HB][P2];
 #pragma unroll
-        for (int i = 0; i < P2; ++i) dA_tile[i] = pair(0.0f, 0.0f);
+            for (int i = 0; i < P2; ++i) h[0][i] = base > 0 ? middle[i] : start[i];
+            // forwards: states and decays, y
 #pragma unroll
-        for (int tu = TB - U; tu >= 0; tu -= U) {
-            float sums1[U], sums2[U];
+            for (int tu = 0; tu < HB; tu += U) {
+                float sums[U];
 #pragma unroll
-            for (int k = U - 1; k >= 0; --k) {
-                const int t = tu + k;
-                const float4 p = s_p[t * CB + cl];
-                f32x2 acc1, acc2;
-                float v[NV];
+                for (int k = 0; k < U; ++k) {
+                    const int t = tu + k;
+                    advance(base + t, h[t], dec[t], h[t + 1]);
+                    f32x2 acc;
 #pragma unroll
-                for (int i = 0; i < P2; ++i) {
-                    const float2 bv = *reinterpret_cast<const float2 *>(&s_b[t * NP + ln * S + 2 * i]);
-                    const float2 cv = *reinterpret_cast<const float2 *>(&s_c[t * NP + ln * S + 2 * i]);
-                    const f32x2 g = fma2(pair(p.z, p.z), pair(cv.x, cv.y), carry[i]);
-                    const float2 db = halves(mul2(g, pair(p.y, p.y))), dc = halves(mul2(h[t + 1][i], pair(p.z, p.z)));
-                    v[2 * i] = db.x;
-                    v[2 * i + 1] = db.y;
-                    v[S + 2 * i] = dc.x;
-                    v[S + 2 * i + 1] = dc.y;
-                    carry[i] = mul2(g, dec[t][i]);
-                    const f32x2 dlog = mul2(carry[i], h[t][i]);
-                    dA_tile[i] = fma2(dlog, pair(p.x, p.x), dA_tile[i]);
-                    acc1 = i == 0 ? mul2(g, pair(bv.x, bv.y)) : fma2(g, pair(bv.x, bv.y), acc1);
-                    acc2 = i == 0 ? mul2(dlog, A2[i]) : fma2(dlog, A2[i], acc2);
-                }
-                const float2 w1 = halves(acc1), w2 = halves(acc2);
-                sums1[k] = w1.x + w1.y;
-                sums2[k] = w2.x + w2.y;
-                // over the warp's channels: lanes that differ above the LN bits
-                int at = 0, nv = NV;
-                bool writes = true;
-#pragma unroll
-                for (int w = 16; w >= LN; w /= 2) {
-                    const bool up = lane & w;
-                    if (nv > 1) {
-                        nv /= 2;
-#pragma unroll
-                        for (int i = 0; i < nv; ++i) {
-                            const float give = up ? v[i] : v[i + nv];
-                            const float keep = up ? v[i + nv] : v[i];
-                            v[i] = keep + __shfl_xor_sync(kFullMask, give, w);
-                        }
-                        at += up ? nv : 0;
-                    } else {
-                        v[0] += __shfl_xor_sync(kFullMask, v[0], w);
-                        writes = writes && !up;
+                    for (int i = 0; i < P2; ++i) {
+                        const float2 cv = *reinterpret_cast<const float2 *>(&s_c[(base + t) * NP + ln * S + 2 * i]);
+                        acc = i == 0 ? mul2(h[t + 1][i], pair(cv.x, cv.y)) : fma2(h[t + 1][i], pair(cv.x, cv.y), acc);
                     }
+                    const float2 v = halves(acc);
+                    sums[k] = v.x + v.y;
                 }
-                constexpr int LEFT = NV > CW ? NV / CW : 1;
-                float *to = s_w + (warp * TB + t) * 2 * NP + ln * NV + at;
-                if (writes)
-#pragma unroll
-                    for (int i = 0; i < LEFT; ++i) to[i] = v[i];
+                if (gate) {
+                    const float v = sum_transposed<U, LN>(sums, lane);
+                    if (LN <= U || ln < U) s_y[(base + tu + ln % U) * YP + cl] = v;
+                }
             }
-            const float v1 = sum_transposed<U, LN>(sums1, lane), v2 = sum_transposed<U, LN>(sums2, lane);
-            if (LN <= U || ln < U) {
-                s_r1[(tu + ln % U) * YP + cl] = v1;
-                s_r2[(tu + ln % U) * YP + cl] = v2;
+            // backwards
+#pragma unroll
+            for (int tu = HB - U; tu >= 0; tu -= U) {
+                float sums1[U], sums2[U];
+#pragma unroll
+                for (int k = U - 1; k >= 0; --k) {
+                    const int t = tu + k;
+                    const float4 p = s_p[(base + t) * CB + cl];
+                    f32x2 acc1, acc2;
+                    float v[NV];
+#pragma unroll
+                    for (int i = 0; i < P2; ++i) {
+                        const float2 bv = *reinterpret_cast<const float2 *>(&s_b[(base + t) * NP + ln * S + 2 * i]);
+                        const float2 cv = *reinterpret_cast<const float2 *>(&s_c[(base + t) * NP + ln * S + 2 * i]);
+                        const f32x2 g = fma2(pair(p.z, p.z), pair(cv.x, cv.y), carry[i]);
+                        const float2 db = halves(mul2(g, pair(p.y, p.y))), dc = halves(mul2(h[t + 1][i], pair(p.z, p.z)));
+                        v[2 * i] = db.x;
+                        v[2 * i + 1] = db.y;
+                        v[S + 2 * i] = dc.x;
+                        v[S + 2 * i + 1] = dc.y;
+                        carry[i] = mul2(g, dec[t][i]);
+                        const f32x2 dlog = mul2(carry[i], h[t][i]);
+                        dA_tile[i] = fma2(dlog, pair(p.x, p.x), dA_tile[i]);
+                        acc1 = i == 0 ? mul2(g, pair(bv.x, bv.y)) : fma2(g, pair(bv.x, bv.y), acc1);
+                        acc2 = i == 0 ? mul2(dlog, A2[i]) : fma2(dlog, A2[i], acc2);
+                    }
+                    const float2 w1 = halves(acc1), w2 = halves(acc2);
+                    sums1[k] = w1.x + w1.y;
+                    sums2[k] = w2.x + w2.y;
+                    // over the warp's channels: lanes that differ above the LN bits
+                    int at = 0, nv = NV;
+                    bool writes = true;
+#pragma unroll
+                    for (int w = 16; w >= LN; w /= 2) {
+                        const bool up = lane & w;
+                        if (nv > 1) {
+                            nv /= 2;
+#pragma unroll
+                            for (int i = 0; i < nv; ++i) {
+                                const float give = up ? v[i] : v[i + nv];
+                                const float keep = up ? v[i + nv] : v[i];
+                                v[i] = keep + __shfl_xor_sync(kFullMask, give, w);
+                            }
+                            at += up ? nv : 0;
+                        } else {
+                            v[0] += __shfl_xor_sync(kFullMask, v[0], w);
+                            writes = writes && !up;
+                        }
+                    }
+                    constexpr int LEFT = NV > CW ? NV / CW : 1;
+                    float *to = s_w + (warp * TB + base + t) * 2 * NP + ln * NV + at;
+                    if (writes)
+#pragma unroll
+                        for (int i = 0; i < LEFT; ++i) to[i] = v[i];
+                }
+                const float v1 = sum_transposed<U, LN>(sums1, lane), v2 = sum_transposed<U, LN>(sums2, lane);
+                if (LN <= U || ln < U) {
+                    s_r1[(base + tu + ln % U) * YP + cl] = v1;
+                    s_r2[(base + tu + ln % U) * YP + cl] = v2;
+                }
             }
         }
 #pragma unroll
@@ -382,7 +407,7 @@ static __global__ void scan_chain_back_kernel(ScanBackArgs b)
     }
 }
 
-// dB and dC: the partial rows of a group's channel blocks, added in order.  One thread per (token, group, lane, value).
+// dB and dC: the partial rows of a group's channel blocks, added in order.  One thread per (token, group, four values).
 template <typename T, int LN, int S>
 __global__ void __launch_bounds__(256) scan_bc_kernel(ScanBackArgs b)
 {
@@ -390,22 +415,31 @@ __global__ void __launch_bounds__(256) scan_bc_kernel(ScanBackArgs b)
     dependent_launch_enter();
     const ScanArgs &a = b.f;
     const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    const int p = static_cast<int>(id % NP2);
-    const long long tg = id / NP2;
+    const int p = static_cast<int>(id % (NP2 / 4)) * 4;
+    const long long tg = id / (NP2 / 4);
     const long long flat = tg / a.groups;
     const int grp = static_cast<int>(tg - flat * a.groups);
     if (flat >= a.map.total) return;
-    const int k = p % (2 * S), n = p / (2 * S) * S + k % S;
-    if (n >= a.states) return;
     const int r = a.map.find(flat);
     if (flat < a.map.first(r) || flat >= a.map.end(r)) return;           // a token of no sequence
     const float *from = b.bc_part + (static_cast<long long>(grp) * a.blocks_per_group * a.map.total + flat) * NP2 + p;
     const long long step = a.map.total * NP2;
-    float v = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
-    for (int i = 0; i < a.blocks_per_group; ++i) v += from[i * step];
-    T *to = token_row<T>(k < S ? b.dB : b.dC, a.map, r, flat) + grp * a.states + n;
-    *to = from_f32<T>(v);
+    for (int i = 0; i < a.blocks_per_group; ++i) {
+        const float4 w = *reinterpret_cast<const float4 *>(from + i * step);
+        v.x += w.x;
+        v.y += w.y;
+        v.z += w.z;
+        v.w += w.w;
+    }
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    T *db = token_row<T>(b.dB, a.map, r, flat) + grp * a.states, *dc = token_row<T>(b.dC, a.map, r, flat) + grp * a.states;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int q = p + i, k = q % (2 * S), n = q / (2 * S) * S + k % S;
+        if (n < a.states) (k < S ? db : dc)[n] = from_f32<T>(f[i]);
+    }
 }
 
 // dA, dD, ddelta_bias: column sums of par_part over sequences and chunks.
@@ -466,7 +500,7 @@ cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *laun
                                       : launch_kernel_smem(scan_backward_kernel<T, LN, S, false>, grid, block, G::bytes(), s, b);
     if (err != cudaSuccess) return err;
     *launches += 1;
-    const long long values = b.f.map.total * b.f.groups * 2 * LN * S;
+    const long long values = b.f.map.total * b.f.groups * (2 * LN * S / 4);
     if (values > 0) {
         err = launch_kernel(scan_bc_kernel<T, LN, S>, dim3(ceil_div(values, 256)), dim3(256), s, b);
         if (err != cudaSuccess) return err;
@@ -506,8 +540,10 @@ cudaError_t launch_scan_backward_t(const sysscan_args &a, cudaStream_t s, int *l
     b.dA = static_cast<float *>(a.dA);
     b.dD = static_cast<float *>(a.dD);
     b.ddbias = static_cast<float *>(a.ddelta_bias);
-    b.bc_part = b.f.carry + p.carry_floats + p.dsum_floats;
+    b.bc_part = static_cast<float *>(a.workspace);                       // read four at a time: first in the workspace
     b.par_part = b.bc_part + p.bc_floats;
+    b.f.carry = b.par_part + p.par_floats;
+    b.f.dsum = b.f.carry + p.carry_floats;
     switch (p.ln * 8 + p.s) {
         case 1 * 8 + 2: return launch_scan_backward_shape<T, 1, 2>(b, s, launches);
         case 2 * 8 + 2: return launch_scan_backward_shape<T, 2, 2>(b, s, launches);

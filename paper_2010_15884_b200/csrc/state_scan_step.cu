@@ -57,7 +57,7 @@ ScanBackPlan scan_backward_plan(const sysscan_args &a)
     const long long warps = (a.seq.sequences * a.channels * p.ln + 31) / 32;
     p.chunks = pick_chunks(warps, a.seq.length, 2 * kSchedulers, 128, &p.chunk);
     const long long total = a.seq.offsets_dev ? a.seq.total : a.seq.sequences * a.seq.length;
-    const long long cb = (p.ln <= 8 ? 128 : (np >= 128 ? 256 : 16 * p.ln)) / p.ln;
+    const long long cb = (p.ln <= 16 || np >= 128 ? 256 : 512) / p.ln;    // channels per block
     const long long blocks = (a.channels / a.groups + cb - 1) / cb * a.groups;
     p.bc_floats = blocks * total * 2 * np;
     p.par_floats = a.seq.sequences * p.chunks * a.channels * (a.states + 2);
