@@ -48,6 +48,29 @@ __device__ __forceinline__ long long saved_base(const SeqMap &m, int r, long lon
     return m.offsets ? first / kScanBlock + r : r * ((m.length + kScanBlock - 1) / kScanBlock);
 }
 
+// Sum of N neighbouring floats in shared memory, by the widest accesses that fit
+template <int N>
+__device__ __forceinline__ float sum_run(const float *p)
+{
+    if constexpr (N == 1) {
+        return p[0];
+    } else if constexpr (N == 2) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        return v.x + v.y;
+    } else {
+        float4 v = *reinterpret_cast<const float4 *>(p);
+#pragma unroll
+        for (int i = 4; i < N; i += 4) {
+            const float4 w = *reinterpret_cast<const float4 *>(p + i);
+            v.x += w.x;
+            v.y += w.y;
+            v.z += w.z;
+            v.w += w.w;
+        }
+        return (v.x + v.y) + (v.z + v.w);
+    }
+}
+
 // A in units of log2; finite, so that tokens past the end, which have d = 0, leave the state alone
 __device__ __forceinline__ float decay_rate(float A)
 {

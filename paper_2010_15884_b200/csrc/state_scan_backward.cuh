@@ -26,7 +26,7 @@ namespace sysconv {
 struct ScanBackArgs {
     ScanArgs f;              // u, delta, z, B, C and the parameters; f.saved is read
     Tokens dy, du, ddelta, dz, dB, dC;
-    float *bc_part;          // [channel block][flat token][lanes][2 S] partial sums of dB and dC
+    float *bc_part;          // [flat token][channel block][2 S][lanes] partial sums of dB (S of them) and dC
     float *par_part;         // [sequence x chunk][channels x states + 2 channels] partial sums of dA, dD, ddelta_bias
     const float *dfinal;
     float *dstate, *dA, *dD, *ddbias;
@@ -45,8 +45,11 @@ struct ScanBackShape {
     static constexpr int VT = PP >= 4 ? 4 : PP;
     static constexpr int BE = TB * NP / NT > 0 ? TB * NP / NT : 1;
     static constexpr int VB = BE >= 4 ? 4 : BE;
-    static constexpr int YP = CB + (LN < 32 ? 32 / LN : 1);
     static constexpr int W = NT / 32;
+    // Sums over the states, up to 8 lanes a channel: every lane leaves its part in shared memory (four words of padding every
+    // 32: no bank conflicts), and the threads that finish a (token, channel) add them; beyond that the lanes exchange them.
+    static constexpr bool PARTS = LN <= 8;
+    static constexpr int YP = PARTS ? W * 36 : CB + (LN < 32 ? 32 / LN : 1);
     static constexpr size_t bytes()
     {
         return sizeof(float) * (TB * CB * 4 + 2 * TB * NP + 3 * TB * YP + W * TB * 2 * NP);
@@ -54,16 +57,19 @@ struct ScanBackShape {
 };
 
 template <typename T, int LN, int S, bool WIDE>
-__global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackShape<LN, S>::NT)) scan_backward_kernel(ScanBackArgs b)
+__global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), (LN <= 2 ? 1 : 512 / ScanBackShape<LN, S>::NT)) scan_backward_kernel(ScanBackArgs b)
 {
     using G = ScanBackShape<LN, S>;
     constexpr int NP = G::NP, NT = G::NT, CB = G::CB, TB = G::TB, HB = G::HB, U = G::U, PP = G::PP, VT = G::VT, BE = G::BE, VB = G::VB;
     constexpr int YP = G::YP, W = G::W, P2 = S / 2, NV = 2 * S, CW = 32 / LN;
     extern __shared__ __align__(16) float smem[];
-    float4 *s_p = reinterpret_cast<float4 *>(smem);                      // [TB][CB] d, d u, dy'
-    float *s_b = smem + TB * CB * 4;                                     // [TB][NP]
-    float *s_c = s_b + TB * NP;
-    float *s_y = s_c + TB * NP;                                          // [TB][YP] each: C.h, r1, r2
+    float4 *s_p = reinterpret_cast<float4 *>(smem);                      // [TB][CB] d, d u, dy', d u
+    // B and C in shared memory: from 16 lanes a channel on as they came (fewer words to read: 4 x 2048 x 512, 64 states
+    // 692 against 752 us), below that as fp32 (fewer instructions: 2048 channels, 16 states 711 against 758 us)
+    using BC = std::conditional_t<(LN >= 16), T, float>;
+    BC *s_b = reinterpret_cast<BC *>(smem + TB * CB * 4);                // [TB][NP]
+    BC *s_c = s_b + TB * NP;
+    float *s_y = smem + TB * CB * 4 + 2 * TB * NP;                       // [TB][YP] each: C.h, r1, r2
     float *s_r1 = s_y + TB * YP, *s_r2 = s_r1 + TB * YP;
     float *s_w = s_r2 + TB * YP;                                         // [W][TB][2 NP]
     dependent_launch_enter();
@@ -80,8 +86,9 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
     const long long t_end = last_chunk ? length : t_begin + a.chunk;
     const long long chain = static_cast<long long>(r) * a.chunks + blockIdx.z;
 
-    const int cl = tid / LN, ln = tid % LN, c = c0 + cl;
+    const int cl = tid / LN, ln = tid % LN, c = c0 + cl;                 // own channel and states
     const bool own = c < c_end;
+    const int n_own = warp * 36 + lane;                                  // place of this lane's parts of the sums over states
     f32x2 A2[P2], carry[P2], dA[P2];
     const bool empty = t_begin >= length && blockIdx.z > 0;              // its parameter sums are zero
     {
@@ -125,7 +132,8 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
         sum_d[j] = sum_b[j] = 0.0f;
     }
     const float *saved = a.saved + (saved_base(a.map, r, first) * a.channels + c) * a.states + ln * S;
-    float *part = b.bc_part + (static_cast<long long>(blockIdx.x) * a.map.total + first) * 2 * NP;
+    const long long part_step = static_cast<long long>(gridDim.x) * 2 * NP;   // between tokens
+    float *part = b.bc_part + first * part_step + blockIdx.x * 2 * NP;
 
     RawTok<T, PP, VT> ru, rd, rz, rg;
     RawTok<T, BE, VB> rb, rc;
@@ -180,7 +188,7 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
                     } else {
                         dyv[q] = dout;
                     }
-                    s_p[tt * CB + pc + j] = make_float4(dv[q], dv[q] * uv[q], dyv[q], 0.0f);
+                    s_p[tt * CB + pc + j] = make_float4(dv[q], dv[q] * uv[q], dyv[q], dv[q] * uv[q]);
                 }
             }
         }
@@ -188,11 +196,8 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
         for (int i = 0; i < BE / VB; ++i) {
             const int e = (i * NT + tid) * VB;
             if (e < TB * NP) {
-#pragma unroll
-                for (int j = 0; j < VB; ++j) {
-                    s_b[e + j] = rb.v[i].get(j);
-                    s_c[e + j] = rc.v[i].get(j);
-                }
+                put_bc<T, VB>(s_b + e, rb.v[i]);
+                put_bc<T, VB>(s_c + e, rc.v[i]);
             }
         }
         f32x2 start[P2], dA_tile[P2];                                    // state before the tile
@@ -207,13 +212,15 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
         // one token forwards: its decay, and the state after it
         auto advance = [&](int t, const f32x2 (&from)[P2], f32x2 (&decay)[P2], f32x2 (&to)[P2]) {
             const float2 d = *reinterpret_cast<const float2 *>(&s_p[t * CB + cl]);
+            const Pack<BC, S> braw = load_pack<BC, S>(s_b + t * NP + ln * S);
 #pragma unroll
             for (int i = 0; i < P2; ++i) {
-                const float2 bv = *reinterpret_cast<const float2 *>(&s_b[t * NP + ln * S + 2 * i]);
+                const float2 bv = make_float2(braw.get(2 * i), braw.get(2 * i + 1));
                 const float2 x = halves(mul2(A2[i], pair(d.x, d.x)));
                 decay[i] = pair(exp2_fast(x.x), exp2_fast(x.y));
                 to[i] = fma2(decay[i], from[i], mul2(pair(bv.x, bv.y), pair(d.y, d.y)));
             }
+            return d.x;
         };
         // The second half of the tile first, from a state that is reached without keeping the way to it: holding all 16 tokens'
         // states and decays would take twice the registers and halve the warps per scheduler.
@@ -228,6 +235,7 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
 #pragma unroll 1
         for (int base = TB - HB; base >= 0; base -= HB) {
             f32x2 h[HB + 1][P2], dec[HB][P2];
+            float step[HB];                                              // d
 #pragma unroll
             for (int i = 0; i < P2; ++i) h[0][i] = base > 0 ? middle[i] : start[i];
             // forwards: states and decays, y
@@ -237,17 +245,19 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
                     const int t = tu + k;
-                    advance(base + t, h[t], dec[t], h[t + 1]);
+                    step[t] = advance(base + t, h[t], dec[t], h[t + 1]);
+                    const Pack<BC, S> craw = load_pack<BC, S>(s_c + (base + t) * NP + ln * S);
                     f32x2 acc;
 #pragma unroll
                     for (int i = 0; i < P2; ++i) {
-                        const float2 cv = *reinterpret_cast<const float2 *>(&s_c[(base + t) * NP + ln * S + 2 * i]);
+                        const float2 cv = make_float2(craw.get(2 * i), craw.get(2 * i + 1));
                         acc = i == 0 ? mul2(h[t + 1][i], pair(cv.x, cv.y)) : fma2(h[t + 1][i], pair(cv.x, cv.y), acc);
                     }
                     const float2 v = halves(acc);
-                    sums[k] = v.x + v.y;
+                    if constexpr (G::PARTS) s_y[(base + t) * YP + n_own] = v.x + v.y;
+                    else sums[k] = v.x + v.y;
                 }
-                if (gate) {
+                if constexpr (!G::PARTS) {
                     const float v = sum_transposed<U, LN>(sums, lane);
                     if (LN <= U || ln < U) s_y[(base + tu + ln % U) * YP + cl] = v;
                 }
@@ -259,28 +269,33 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
 #pragma unroll
                 for (int k = U - 1; k >= 0; --k) {
                     const int t = tu + k;
-                    const float4 p = s_p[(base + t) * CB + cl];
+                    const float2 p = *(reinterpret_cast<const float2 *>(&s_p[(base + t) * CB + cl]) + 1);     // dy', d u
+                    const Pack<BC, S> braw = load_pack<BC, S>(s_b + (base + t) * NP + ln * S), craw = load_pack<BC, S>(s_c + (base + t) * NP + ln * S);
                     f32x2 acc1, acc2;
                     float v[NV];
 #pragma unroll
                     for (int i = 0; i < P2; ++i) {
-                        const float2 bv = *reinterpret_cast<const float2 *>(&s_b[(base + t) * NP + ln * S + 2 * i]);
-                        const float2 cv = *reinterpret_cast<const float2 *>(&s_c[(base + t) * NP + ln * S + 2 * i]);
-                        const f32x2 g = fma2(pair(p.z, p.z), pair(cv.x, cv.y), carry[i]);
-                        const float2 db = halves(mul2(g, pair(p.y, p.y))), dc = halves(mul2(h[t + 1][i], pair(p.z, p.z)));
+                        const float2 bv = make_float2(braw.get(2 * i), braw.get(2 * i + 1)), cv = make_float2(craw.get(2 * i), craw.get(2 * i + 1));
+                        const f32x2 g = fma2(pair(p.x, p.x), pair(cv.x, cv.y), carry[i]);
+                        const float2 db = halves(mul2(g, pair(p.y, p.y))), dc = halves(mul2(h[t + 1][i], pair(p.x, p.x)));
                         v[2 * i] = db.x;
                         v[2 * i + 1] = db.y;
                         v[S + 2 * i] = dc.x;
                         v[S + 2 * i + 1] = dc.y;
                         carry[i] = mul2(g, dec[t][i]);
                         const f32x2 dlog = mul2(carry[i], h[t][i]);
-                        dA_tile[i] = fma2(dlog, pair(p.x, p.x), dA_tile[i]);
+                        dA_tile[i] = fma2(dlog, pair(step[t], step[t]), dA_tile[i]);
                         acc1 = i == 0 ? mul2(g, pair(bv.x, bv.y)) : fma2(g, pair(bv.x, bv.y), acc1);
                         acc2 = i == 0 ? mul2(dlog, A2[i]) : fma2(dlog, A2[i], acc2);
                     }
                     const float2 w1 = halves(acc1), w2 = halves(acc2);
-                    sums1[k] = w1.x + w1.y;
-                    sums2[k] = w2.x + w2.y;
+                    if constexpr (G::PARTS) {
+                        s_r1[(base + t) * YP + n_own] = w1.x + w1.y;
+                        s_r2[(base + t) * YP + n_own] = w2.x + w2.y;
+                    } else {
+                        sums1[k] = w1.x + w1.y;
+                        sums2[k] = w2.x + w2.y;
+                    }
                     // over the warp's channels: lanes that differ above the LN bits
                     int at = 0, nv = NV;
                     bool writes = true;
@@ -302,15 +317,17 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
                         }
                     }
                     constexpr int LEFT = NV > CW ? NV / CW : 1;
-                    float *to = s_w + (warp * TB + base + t) * 2 * NP + ln * NV + at;
+                    float *to = s_w + (warp * TB + base + t) * 2 * NP + ln;
                     if (writes)
 #pragma unroll
-                        for (int i = 0; i < LEFT; ++i) to[i] = v[i];
+                        for (int i = 0; i < LEFT; ++i) to[(at + i) * LN] = v[i];
                 }
-                const float v1 = sum_transposed<U, LN>(sums1, lane), v2 = sum_transposed<U, LN>(sums2, lane);
-                if (LN <= U || ln < U) {
-                    s_r1[(base + tu + ln % U) * YP + cl] = v1;
-                    s_r2[(base + tu + ln % U) * YP + cl] = v2;
+                if constexpr (!G::PARTS) {
+                    const float v1 = sum_transposed<U, LN>(sums1, lane), v2 = sum_transposed<U, LN>(sums2, lane);
+                    if (LN <= U || ln < U) {
+                        s_r1[(base + tu + ln % U) * YP + cl] = v1;
+                        s_r2[(base + tu + ln % U) * YP + cl] = v2;
+                    }
                 }
             }
         }
@@ -326,12 +343,14 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
                 float odu[VT], odd[VT], odz[VT];
 #pragma unroll
                 for (int j = 0; j < VT; ++j) {
-                    const int q = i * VT + j, at = tt * YP + pc + j;
-                    const float r1 = s_r1[at], r2 = s_r2[at] * 0.69314718055994531f;      // A2 is A log2(e)
+                    const int q = i * VT + j, cc = pc + j;
+                    const int at = tt * YP + (G::PARTS ? cc * LN + cc * LN / 32 * 4 : cc);
+                    constexpr int RUN = G::PARTS ? LN : 1;
+                    const float r1 = sum_run<RUN>(s_r1 + at), r2 = sum_run<RUN>(s_r2 + at) * 0.69314718055994531f;   // A2 is A log2(e)
                     const float dd = fmaf(uv[q], r1, r2) * slope[q];
                     odu[j] = fmaf(dv[q], r1, dyv[q] * dskip[j]);
                     odd[j] = dd;
-                    if (gate) odz[j] = fmaf(dskip[j], uv[q], s_y[at]) * zf[q];
+                    if (gate) odz[j] = fmaf(dskip[j], uv[q], sum_run<RUN>(s_y + at)) * zf[q];
                     sum_b[j] += dd;
                     sum_d[j] = fmaf(dyv[q], uv[q], sum_d[j]);
                 }
@@ -344,7 +363,7 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), 512 / (ScanBackSha
             float v = 0.0f;
 #pragma unroll
             for (int w = 0; w < W; ++w) v += s_w[w * TB * 2 * NP + e];
-            if (t0 + e / (2 * NP) < t_end) part[t0 * 2 * NP + e] = v;
+            if (t0 + e / (2 * NP) < t_end) part[(t0 + e / (2 * NP)) * part_step + e % (2 * NP)] = v;
         }
     }
 
@@ -407,37 +426,44 @@ static __global__ void scan_chain_back_kernel(ScanBackArgs b)
     }
 }
 
-// dB and dC: the partial rows of a group's channel blocks, added in order.  One thread per (token, group, four values).
+// dB and dC: the partial rows of a group's channel blocks, added in a fixed order.  A token's rows are contiguous; ROWS threads
+// share each run of four values, every ROWS-th row each, and join by exchanges.
 template <typename T, int LN, int S>
 __global__ void __launch_bounds__(256) scan_bc_kernel(ScanBackArgs b)
 {
-    constexpr int NP2 = 2 * LN * S;
+    constexpr int NP2 = 2 * LN * S, WIDTH = NP2 / 4;                     // threads per row
+    constexpr int ROWS = WIDTH >= 32 ? 1 : 32 / WIDTH;
     dependent_launch_enter();
     const ScanArgs &a = b.f;
     const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    const int p = static_cast<int>(id % (NP2 / 4)) * 4;
-    const long long tg = id / (NP2 / 4);
+    const int p = static_cast<int>(id % WIDTH) * 4, row = static_cast<int>(id / WIDTH % ROWS);
+    const long long tg = id / (WIDTH * ROWS);
     const long long flat = tg / a.groups;
     const int grp = static_cast<int>(tg - flat * a.groups);
-    if (flat >= a.map.total) return;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (flat < a.map.total) {
+        const float *from = b.bc_part + (flat * a.groups + grp) * a.blocks_per_group * NP2 + p;
+#pragma unroll 4
+        for (int i = row; i < a.blocks_per_group; i += ROWS) {
+            const float4 w = *reinterpret_cast<const float4 *>(from + i * NP2);
+            v.x += w.x;
+            v.y += w.y;
+            v.z += w.z;
+            v.w += w.w;
+        }
+    }
+    float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int w = WIDTH; w < 32; w *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] += __shfl_xor_sync(kFullMask, f[i], w);
+    if (flat >= a.map.total || row > 0) return;
     const int r = a.map.find(flat);
     if (flat < a.map.first(r) || flat >= a.map.end(r)) return;           // a token of no sequence
-    const float *from = b.bc_part + (static_cast<long long>(grp) * a.blocks_per_group * a.map.total + flat) * NP2 + p;
-    const long long step = a.map.total * NP2;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int i = 0; i < a.blocks_per_group; ++i) {
-        const float4 w = *reinterpret_cast<const float4 *>(from + i * step);
-        v.x += w.x;
-        v.y += w.y;
-        v.z += w.z;
-        v.w += w.w;
-    }
-    const float f[4] = {v.x, v.y, v.z, v.w};
     T *db = token_row<T>(b.dB, a.map, r, flat) + grp * a.states, *dc = token_row<T>(b.dC, a.map, r, flat) + grp * a.states;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int q = p + i, k = q % (2 * S), n = q / (2 * S) * S + k % S;
+        const int q = p + i, k = q / LN, n = q % LN * S + k % S;
         if (n < a.states) (k < S ? db : dc)[n] = from_f32<T>(f[i]);
     }
 }
@@ -500,7 +526,8 @@ cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *laun
                                       : launch_kernel_smem(scan_backward_kernel<T, LN, S, false>, grid, block, G::bytes(), s, b);
     if (err != cudaSuccess) return err;
     *launches += 1;
-    const long long values = b.f.map.total * b.f.groups * (2 * LN * S / 4);
+    constexpr int width = 2 * LN * S / 4;
+    const long long values = b.f.map.total * b.f.groups * width * (width >= 32 ? 1 : 32 / width);
     if (values > 0) {
         err = launch_kernel(scan_bc_kernel<T, LN, S>, dim3(ceil_div(values, 256)), dim3(256), s, b);
         if (err != cudaSuccess) return err;
