@@ -94,7 +94,7 @@ __device__ __forceinline__ int pass_empty(const CausalArgs &a, int r, long long 
     return r;
 }
 
-constexpr int kAhead = 4;                // tokens per step of a thread
+constexpr int kAhead = 2;                // tokens per step of a thread
 
 // A thread's input rows, kAhead at a time, STAGES - 1 steps ahead in its own part of shared memory (types and widths that
 // asynchronous copies do not have are loaded when they are needed).
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) causal_kernel(CausalArgs a)
 constexpr int kBackRows = 4;             // runs per block, 32 threads (groups of V channels) each
 
 template <typename T, int V, int K>
-__global__ void __launch_bounds__(32 * kBackRows) causal_backward_kernel(CausalArgs a)
+__global__ void __launch_bounds__(32 * kBackRows, 4) causal_backward_kernel(CausalArgs a)
 {
     dependent_launch_enter();
     constexpr int U = kAhead, STAGES = Stages<T, V>::value;
@@ -513,7 +513,7 @@ long long backward_runs(const sysconv_causal_args &a, int v, int *run)
 {
     const long long total = a.seq.offsets_dev ? a.seq.total : a.seq.sequences * a.seq.length;
     const long long groups = (a.channels + v - 1) / v;
-    *run = run_length(total, (groups + 31) / 32 * 32, 3);
+    *run = run_length(total, (groups + 31) / 32 * 32, 4);
     const long long least = total / (65535LL * kBackRows) + 1;          // the grid's rows are limited
     if (*run < least) *run = static_cast<int>(least);
     const long long runs = (total + *run - 1) / *run;
