@@ -9,6 +9,11 @@ The compute lives in ``libsysconv.so`` (CUDA, C ABI, see ``include/sysconv.h``);
 ``binding`` is a thin ctypes layer over it.  There is no CPU fallback: every
 call fails loudly when the library is missing.  ``inputs`` only draws the
 seeded synthetic workloads.
+
+``sequence`` holds what a sequence model puts beside a convolution: causal
+convolution with carried state, selective state space scan and group norm, each
+for prompts, training and single tokens (``include/sysconv_sequence.h``);
+``scanblock`` puts them together.
 """
 
 _BINDING_NAMES = (
@@ -19,8 +24,17 @@ _BINDING_NAMES = (
     "launch_count", "device_status",
 )
 
+# the sequence operators (sequence.py)
+_SEQUENCE_NAMES = (
+    "conv1d_causal", "conv1d_causal_backward", "conv1d_causal_step", "state_scan", "state_scan_backward", "state_scan_step",
+    "groupnorm", "groupnorm_backward", "ScanGrads",
+)
+
 
 def __getattr__(name):
+    if name in _SEQUENCE_NAMES:
+        from . import sequence
+        return getattr(sequence, name)
     if name in _BINDING_NAMES:
         from . import binding
         return getattr(binding, name)

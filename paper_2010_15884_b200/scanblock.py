@@ -1,0 +1,176 @@
+"""A gated convolution-scan block on the sequence operators: what they are used for, put together.
+
+    x -> group norm per token -> projection to (u, z) -> causal convolution + silu of u -> projections to (delta, B, C)
+      -> state space scan of u, gated by silu(z) -> projection -> + x
+
+``ScanBlock`` runs it for whole sequences (dense or packed, differentiable), for prompts with the states carried on, and token by
+token from a cache of states.  The projections are plain matrix products of PyTorch; everything else is ``sequence``.
+
+``python -m paper_2010_15884_b200.scanblock`` (on a GPU) takes a few training steps, reads a prompt, continues it token by
+token and compares the continuation with the prompt form.
+"""
+import math
+
+import torch
+
+from . import sequence as seq
+
+
+class _Conv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, offsets):
+        ctx.save_for_backward(x, weight, bias)
+        ctx.offsets = offsets
+        return seq.conv1d_causal(x, weight, bias, "silu", offsets=offsets)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, bias = ctx.saved_tensors
+        return seq.conv1d_causal_backward(dy.contiguous(), x, weight, bias, "silu", offsets=ctx.offsets)[:3] + (None,)
+
+
+class _Scan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, u, delta, A, B, C, D, z, bias, offsets, longest):
+        y, saved = seq.state_scan(u, delta, A, B, C, D=D, z=z, delta_bias=bias, softplus=True, offsets=offsets, longest=longest,
+                                  save=True)
+        ctx.save_for_backward(u, delta, A, B, C, D, z, bias, saved)
+        ctx.how = dict(softplus=True, offsets=offsets, longest=longest)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        u, delta, A, B, C, D, z, bias, saved = ctx.saved_tensors
+        g = seq.state_scan_backward(dy.contiguous(), u, delta, A, B, C, saved, D=D, z=z, delta_bias=bias, **ctx.how)
+        return g.du, g.ddelta, g.dA, g.dB, g.dC, g.dD, g.dz, g.ddelta_bias, None, None
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, groups, weight, bias):
+        y, mean, rstd = seq.groupnorm(x, groups, weight, bias, return_stats=True)
+        ctx.save_for_backward(x, mean, rstd, weight, bias)
+        ctx.groups = groups
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, mean, rstd, weight, bias = ctx.saved_tensors
+        dx, dw, db = seq.groupnorm_backward(dy.contiguous(), x, ctx.groups, mean, rstd, weight, bias)
+        return dx, None, dw, db
+
+
+class ScanBlock(torch.nn.Module):
+    """width: channels of the stream; channels: inside the block; states per channel; taps of the convolution; groups of the norm."""
+
+    def __init__(self, width, channels, states=16, taps=4, groups=8, rank=None, dtype=torch.bfloat16, device="cuda"):
+        super().__init__()
+        self.channels, self.states, self.taps, self.groups = channels, states, taps, groups
+        self.rank = rank or max(1, width // 16)
+        new = dict(dtype=dtype, device=device)
+        f32 = dict(dtype=torch.float32, device=device)
+
+        def matrix(rows, columns):
+            return torch.nn.Parameter(torch.randn(rows, columns, **new) / math.sqrt(columns))
+
+        self.norm_weight = torch.nn.Parameter(torch.ones(width, **f32))
+        self.norm_bias = torch.nn.Parameter(torch.zeros(width, **f32))
+        self.into = matrix(2 * channels, width)
+        self.conv_weight = torch.nn.Parameter(torch.randn(channels, taps, **new) / math.sqrt(taps))
+        self.conv_bias = torch.nn.Parameter(torch.zeros(channels, **new))
+        self.params = matrix(self.rank + 2 * states, channels)
+        self.widen = matrix(channels, self.rank)
+        step = torch.exp(torch.rand(channels, **f32) * math.log(100.0) + math.log(1e-3))      # softplus(bias) in [0.001, 0.1]
+        self.delta_bias = torch.nn.Parameter(step + torch.log(-torch.expm1(-step)))
+        self.log_A = torch.nn.Parameter(torch.log(torch.arange(1, states + 1, **f32)).repeat(channels, 1))
+        self.D = torch.nn.Parameter(torch.ones(channels, **f32))
+        self.out = matrix(width, channels)
+
+    def _project(self, u):
+        """delta, B, C of the convolution's outputs; B and C stay views of one projection."""
+        p = u @ self.params.t()
+        return p[..., : self.rank] @ self.widen.t(), p[..., self.rank: self.rank + self.states], p[..., self.rank + self.states:]
+
+    def _token_norm(self, x, norm):
+        rows = x.reshape(-1, 1, x.shape[-1])                               # every token is a batch entry of its own
+        return norm(rows).reshape(x.shape)
+
+    def forward(self, x, offsets=None, longest=None):
+        """Whole sequences from empty states: x (batch, length, width), or packed (tokens, width) with offsets."""
+        h = self._token_norm(x, lambda v: _Norm.apply(v, self.groups, self.norm_weight, self.norm_bias)) @ self.into.t()
+        u, z = h[..., : self.channels], h[..., self.channels:]
+        u = _Conv.apply(u, self.conv_weight, self.conv_bias, offsets)
+        delta, B, C = self._project(u)
+        y = _Scan.apply(u, delta, -torch.exp(self.log_A), B, C, self.D, z, self.delta_bias, offsets, longest)
+        return x + y @ self.out.t()
+
+    def new_cache(self, slots):
+        """Empty states of `slots` sequences: of the convolution and of the scan."""
+        kind, device = self.into.dtype, self.into.device
+        return (torch.zeros(slots, self.taps - 1, self.channels, dtype=kind, device=device),
+                torch.zeros(slots, self.channels, self.states, dtype=torch.float32, device=device))
+
+    @torch.no_grad()
+    def prompt(self, x, cache, slots, offsets=None, longest=None):
+        """Sequences that go on from their slots' states, which are left after the last token.  slots: int32, one per sequence."""
+        norm = lambda v: seq.groupnorm(v, self.groups, self.norm_weight, self.norm_bias)   # noqa: E731
+        h = self._token_norm(x, norm) @ self.into.t()
+        at = slots.long()
+        u, conv = seq.conv1d_causal(h[..., : self.channels], self.conv_weight, self.conv_bias, "silu", state=cache[0][at],
+                                    offsets=offsets, return_state=True)
+        delta, B, C = self._project(u)
+        y, state = seq.state_scan(u, delta, -torch.exp(self.log_A), B, C, D=self.D, z=h[..., self.channels:],
+                                  delta_bias=self.delta_bias, softplus=True, state=cache[1][at], offsets=offsets, longest=longest,
+                                  return_state=True)
+        cache[0][at], cache[1][at] = conv, state
+        return x + y @ self.out.t()
+
+    @torch.no_grad()
+    def step(self, x, cache, slots):
+        """One token of each row, x (rows, width); the slots' states are updated in place (a slot of -1: an idle row)."""
+        norm = lambda v: seq.groupnorm(v, self.groups, self.norm_weight, self.norm_bias)   # noqa: E731
+        h = self._token_norm(x, norm) @ self.into.t()
+        u = seq.conv1d_causal_step(h[:, : self.channels], cache[0], self.conv_weight, self.conv_bias, "silu", slots=slots)
+        delta, B, C = self._project(u)
+        y = seq.state_scan_step(u, delta, -torch.exp(self.log_A), B, C, cache[1], D=self.D, z=h[:, self.channels:],
+                                delta_bias=self.delta_bias, softplus=True, slots=slots)
+        return x + y @ self.out.t()
+
+
+def main():
+    torch.manual_seed(0)
+    block = ScanBlock(width=256, channels=512, dtype=torch.float32)
+    lengths = [37, 0, 64, 5]
+    offsets = torch.tensor([0] + [sum(lengths[: i + 1]) for i in range(4)], dtype=torch.int32, device="cuda")
+    x = torch.randn(sum(lengths), 256, device="cuda")
+    target = torch.randn_like(x)
+    optimizer = torch.optim.SGD(block.parameters(), lr=0.1)
+    for i in range(5):
+        optimizer.zero_grad()
+        loss = (block(x, offsets, max(lengths)) - target).square().mean()
+        loss.backward()
+        optimizer.step()
+        print("training step %d: loss %.5f" % (i, float(loss.detach())))
+    with torch.no_grad():
+        whole = block(x, offsets, max(lengths))
+    # the same packed sequences as prompts of all but their last five tokens (the short ones: none), then token by token
+    head = [max(0, n - 5) for n in lengths]
+    cache, slots = block.new_cache(6), torch.tensor([4, 0, 2, 5], dtype=torch.int32, device="cuda")
+    first = [int(v) for v in offsets[:-1]]
+    rows = torch.cat([torch.arange(a, a + n, device="cuda") for a, n in zip(first, head)])
+    ends = torch.tensor([0] + [sum(head[: i + 1]) for i in range(4)], dtype=torch.int32, device="cuda")
+    got = torch.empty_like(whole)
+    got[rows] = block.prompt(x[rows], cache, slots, ends, max(head))
+    for t in range(5):
+        live = torch.tensor([s if n else -1 for s, n in zip(slots.tolist(), lengths)], dtype=torch.int32, device="cuda")
+        at = torch.tensor([a + h + t if n else 0 for a, h, n in zip(first, head, lengths)], device="cuda")
+        y = block.step(x[at], cache, live)
+        keep = live >= 0
+        got[at[keep]] = y[keep]
+    off = float((got - whole).norm() / whole.norm())
+    print("prompt and single tokens against whole sequences: relative difference %.2e" % off)
+    return off
+
+
+if __name__ == "__main__":
+    main()

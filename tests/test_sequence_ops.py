@@ -619,3 +619,63 @@ def test_nothing_to_do(cuda_device):
     g = seq.state_scan_backward(none, none, none, A, B, B, saved, offsets=off, dfinal=df, state_grad=True)
     assert torch.equal(g.dstate, df) and (g.dA == 0).all()
     assert seq.groupnorm(torch.zeros(0, 4, 8, device="cuda"), 2).shape == (0, 4, 8)
+
+
+# ------------------------------------------------------------------------------------------ the block that uses them together
+
+
+def test_block_trains_and_continues_prompts(cuda_device):
+    """Gradients of the block against the same block in torch's own operators in 64 bits, fp32 matrix products included
+    (1e-4 of the 2-norm); prompt and single tokens against whole sequences (fp32, 1e-5)."""
+    from paper_2010_15884_b200 import scanblock
+    before = torch.backends.cuda.matmul.allow_tf32
+    torch.backends.cuda.matmul.allow_tf32 = False
+    try:
+        assert scanblock.main() <= 1e-5
+        torch.manual_seed(1)
+        b = scanblock.ScanBlock(width=48, channels=40, states=8, groups=4, dtype=torch.float32)
+        x = torch.randn(2, 23, 48, device="cuda", requires_grad=True)
+        dy = torch.randn(2, 23, 48, device="cuda")
+        b(x).backward(dy)
+        p = {k: v.detach().double().requires_grad_() for k, v in b.named_parameters()}
+        xd = x.detach().double().requires_grad_()
+        f = torch.nn.functional
+        h = f.group_norm(xd.reshape(-1, 48), 4, p["norm_weight"], p["norm_bias"], 1e-5).reshape(xd.shape) @ p["into"].t()
+        u, z = h[..., :40], h[..., 40:]
+        u = f.silu(f.conv1d(f.pad(u.transpose(1, 2), (3, 0)), p["conv_weight"][:, None], p["conv_bias"], groups=40).transpose(1, 2))
+        q = u @ p["params"].t()
+        B, C = q[..., b.rank: b.rank + 8], q[..., b.rank + 8:]
+        v = dict(u=u, delta=q[..., : b.rank] @ p["widen"].t(), z=z, B=B[:, :, None], C=C[:, :, None])
+        y, _ = _loop64(v, dict(A=-torch.exp(p["log_A"]), D=p["D"], delta_bias=p["delta_bias"]), torch.zeros(2, 40, 8, device="cuda"), True)
+        (xd + y @ p["out"].t()).backward(dy.double())
+        for name, t in b.named_parameters():
+            assert float((t.grad.double() - p[name].grad).norm() / p[name].grad.norm()) <= 1e-4, name
+        assert float((x.grad.double() - xd.grad).norm() / xd.grad.norm()) <= 1e-4
+    finally:
+        torch.backends.cuda.matmul.allow_tf32 = before
+
+
+def test_python_and_native_marshalling_agree(cuda_device, monkeypatch):
+    """The calls by way of the C++ module and by way of the Python layer alone give the same bits."""
+    assert seq._sequence is not None, "_sequence.so is not built"
+    case = ("bf16", [5, 0, 33], 24, 16, 2, True, True, True, True, True, True)
+    v, p, dy, st, plus, off = scan_case(case, 9)
+    x, w, b = v["u"], Draw(1, torch.bfloat16)(24, 4), Draw(2, torch.bfloat16)(24)
+    cs, nw = Draw(3, torch.bfloat16)(3, 3, 24), Draw(4, torch.float32)(24)
+
+    def everything():
+        y, final, saved = seq.state_scan(**v, **p, softplus=plus, state=st, offsets=off, return_state=True, save=True)
+        g = seq.state_scan_backward(dy, saved=saved, **v, **p, softplus=plus, offsets=off, dfinal=final, state_grad=True)
+        h, c = st.clone(), cs.clone()
+        rows = {k: t[:3] for k, t in v.items()}
+        ys = seq.state_scan_step(rows["u"], rows["delta"], p["A"], rows["B"], rows["C"], h, D=p["D"], z=rows["z"], softplus=True)
+        yc = seq.conv1d_causal_step(x[:3], c, w, b, "silu")
+        yn, mean, rstd = seq.groupnorm(x[None], 3, nw, nw, activation="silu", return_stats=True)
+        # (`saved` itself has rows between packed sequences that nobody writes or reads)
+        return (y, final, *g, h, c, ys, yc, yn, mean, rstd, *seq.conv1d_causal(x, w, b, "silu", cs, off, True),
+                *seq.conv1d_causal_backward(dy, x, w, b, "silu", cs, off, cs), *seq.groupnorm_backward(dy[None], x[None], 3, mean, rstd, nw, nw, "silu"))
+
+    native = everything()
+    monkeypatch.setattr(seq, "_sequence", None)
+    for a, c in zip(native, everything()):
+        assert torch.equal(a, c)
