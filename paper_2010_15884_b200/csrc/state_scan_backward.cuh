@@ -216,7 +216,7 @@ __global__ void __launch_bounds__((ScanBackShape<LN, S>::NT), (LN <= 2 ? 1 : 512
 #pragma unroll
             for (int i = 0; i < P2; ++i) {
                 const float2 bv = make_float2(braw.get(2 * i), braw.get(2 * i + 1));
-                const float2 x = halves(mul2(A2[i], pair(d.x, d.x)));
+                const float2 x = halves(fma2(A2[i], pair(d.x, d.x), pair(kDecayOffset, kDecayOffset)));
                 decay[i] = pair(exp2_fast(x.x), exp2_fast(x.y));
                 to[i] = fma2(decay[i], from[i], mul2(pair(bv.x, bv.y), pair(d.y, d.y)));
             }

@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(StepArgs a)
             float acc = 0.0f, hn[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                hn[i] = fmaf(exp2_fast(dt * (av[k].get(i) * kLog2e)), h[k].get(i), dut * bv[i]);
+                hn[i] = fmaf(exp2_fast(fmaf(dt, av[k].get(i) * kLog2e, kDecayOffset)), h[k].get(i), dut * bv[i]);
                 if (i < valid_n) acc = fmaf(hn[i], cv[i], acc);
             }
             store_some<float, 4>(st + static_cast<long long>(ct) * a.states, hn, ct < a.channels ? valid_n : 0, a.wide);
