@@ -380,23 +380,24 @@ __global__ void __launch_bounds__(32 * kBackRows, 4) causal_backward_kernel(Caus
     }
 }
 
-// dweight and dbias: column sums of the partial rows.  A block takes 32 columns (of (K+1) x channels) and 32 row slices.
+// dweight and dbias: column sums of the partial rows.  A block takes 32 columns (of (K+1) x channels) and 8 row slices.
 template <typename W>
-__global__ void __launch_bounds__(1024) causal_reduce_kernel(const float *partial, long long rows, int channels, int taps, W *dweight, W *dbias)
+__global__ void __launch_bounds__(256) causal_reduce_kernel(const float *partial, long long rows, int channels, int taps, W *dweight, W *dbias)
 {
     dependent_launch_enter();
-    __shared__ float sums[32][33];
+    __shared__ float sums[8][33];
     const long long columns = static_cast<long long>(taps + 1) * channels;
     const long long col = static_cast<long long>(blockIdx.x) * 32 + threadIdx.x;
     float v = 0.0f;
     if (col < columns)
-        for (long long r = threadIdx.y; r < rows; r += 32) v += partial[r * columns + col];
+#pragma unroll 4
+        for (long long r = threadIdx.y; r < rows; r += 8) v += partial[r * columns + col];
     sums[threadIdx.y][threadIdx.x] = v;
     __syncthreads();
     if (threadIdx.y != 0 || col >= columns) return;
     v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v += sums[i][threadIdx.x];
+    for (int i = 0; i < 8; ++i) v += sums[i][threadIdx.x];
     const int k = static_cast<int>(col / channels), c = static_cast<int>(col % channels);
     if (k < taps) {
         if (dweight != nullptr) dweight[static_cast<long long>(c) * taps + k] = from_f32<W>(v);
@@ -583,7 +584,7 @@ cudaError_t launch_causal_backward(const sysconv_causal_args &a, cudaStream_t s,
         });
     });
     if (err != cudaSuccess || !params) return err;
-    const dim3 grid(ceil_div((a.taps + 1) * a.channels, 32)), block(32, 32);
+    const dim3 grid(ceil_div((a.taps + 1) * a.channels, 32)), block(32, 8);
     *launches += 1;
     const int taps = static_cast<int>(a.taps);
     return with_type(a.weight_type, [&](auto *tag) {
