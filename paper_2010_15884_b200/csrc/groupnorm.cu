@@ -729,30 +729,32 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_join_kernel(NormArgs a
     }
 }
 
-// dweight, dbias: sums over the rows of pq.  32 channels x 32 row slices a block.
-__global__ void __launch_bounds__(1024) norm_param_kernel(const float *pq, long long rows, int channels, float *dweight, float *dbias)
+// dweight, dbias: sums over the rows of pq.  8 channels x 64 row slices a block: there may be few channels and many rows.
+constexpr int kParamSlices = 64;
+__global__ void __launch_bounds__(8 * kParamSlices) norm_param_kernel(const float *pq, long long rows, int channels, float *dweight, float *dbias)
 {
     dependent_launch_enter();
-    __shared__ float s1[32][33], s2[32][33];
-    const int c = blockIdx.x * 32 + threadIdx.x;
-    float v1 = 0.0f, v2 = 0.0f;
+    __shared__ float2 sums[kParamSlices][8];
+    const int c = blockIdx.x * 8 + threadIdx.x;
+    float2 v = make_float2(0.0f, 0.0f);
     if (c < channels)
-        for (long long r = threadIdx.y; r < rows; r += 32) {
-            v1 += pq[r * 2 * channels + c];
-            v2 += pq[(r * 2 + 1) * channels + c];
+#pragma unroll 4
+        for (long long r = threadIdx.y; r < rows; r += kParamSlices) {
+            v.x += pq[r * 2 * channels + c];
+            v.y += pq[(r * 2 + 1) * channels + c];
         }
-    s1[threadIdx.y][threadIdx.x] = v1;
-    s2[threadIdx.y][threadIdx.x] = v2;
-    __syncthreads();
-    if (threadIdx.y != 0 || c >= channels) return;
-    v1 = v2 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        v1 += s1[i][threadIdx.x];
-        v2 += s2[i][threadIdx.x];
+    sums[threadIdx.y][threadIdx.x] = v;
+    for (int half = kParamSlices / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (threadIdx.y < half) {
+            v.x += sums[threadIdx.y + half][threadIdx.x].x;
+            v.y += sums[threadIdx.y + half][threadIdx.x].y;
+            sums[threadIdx.y][threadIdx.x] = v;
+        }
     }
-    if (dbias) dbias[c] = v1;
-    if (dweight) dweight[c] = v2;
+    if (threadIdx.y != 0 || c >= channels) return;
+    if (dbias) dbias[c] = v.x;
+    if (dweight) dweight[c] = v.y;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -1007,7 +1009,7 @@ cudaError_t launch_groupnorm_backward(const sysgroupnorm_args &a, cudaStream_t s
     if (err != cudaSuccess || !params) return err;
     *launches += 1;
     const long long rows = p.q > 0 ? p.blocks : a.batch;
-    return launch_kernel(norm_param_kernel, dim3(ceil_div(a.channels, 32)), dim3(32, 32), s, k.pq, rows, k.channels,
+    return launch_kernel(norm_param_kernel, dim3(ceil_div(a.channels, 8)), dim3(8, kParamSlices), s, k.pq, rows, k.channels,
                          static_cast<float *>(a.dweight), static_cast<float *>(a.dbias));
 }
 

@@ -7,23 +7,36 @@ namespace {
 
 constexpr long long kSchedulers = 148 * 4;
 
-// Chunks per sequence.  `warps` = warps of the unsplit grid; a chunk costs a second pass over its tokens, so tokens are split
-// only while the machine would be mostly idle, into `target` warps, and never finer than 128 tokens.  Forward, 8192 tokens and
-// 16 states, by channels, whole against split: 256: 198 / 48 us, 1024: 237 / 132, 1408: 240 / 165, 2048: 243 / 242;
-// training step: 256: 1818 / 150 us, 768: 1852 / 362.
-int pick_chunks(long long warps, long long length, long long target, int *chunk)
+// Chunks per sequence.  `warps` = warps that one sequence takes unsplit.  A chunk costs a second pass over its tokens, so tokens
+// are split only while the machine would be mostly idle, into chunks that fill four warps a scheduler.  8192 tokens and 16 states,
+// by channels, whole against split, forward: 256: 198 / 48 us, 1024: 237 / 132, 1408: 240 / 165, 2048: 243 / 242; training step:
+// 256: 1818 / 151, 768: 1852 / 362; with six or eight warps a scheduler 256 channels take 176 or 183 us.
+// Never finer than `least` tokens: forward 128, backward 32, where a token takes longer (300 tokens of 2000 channels forward:
+// 10.6 us whole, 20 in chunks of 32; training step of 342 tokens of 432 channels: 78 whole, 51 in chunks of 32).
+// Sequences may differ in length, so the chunk follows from all tokens, less one part-filled chunk per sequence (four packed
+// sequences, 2048 tokens of 768 channels, training step: 175 us from the longest one alone, 126 so).  The grid and the workspace
+// have a place for each (sequence, chunk), used or not, and stay within four times the target.
+int pick_chunks(long long warps, const sysconv_sequences &seq, long long total, long long least, int *chunk)
 {
-    constexpr long long least = 128;
+    constexpr long long kTarget = 4 * kSchedulers;
     *chunk = 1 << 30;
-    if (warps * 3 > 4 * kSchedulers || length < 2 * least) return 1;
-    long long n = target / warps;
-    if (n > length / least) n = length / least;
+    const long long longest = seq.length;
+    if (total * warps * 3 > kTarget * longest || longest < 3 * least) return 1;
+    const long long slots = kTarget / warps;
+    const long long whole = slots - (seq.sequences - 1);
+    const long long share = whole * 2 > slots ? whole : (slots + 1) / 2;
+    long long c = (total + share - 1) / share;
+    if (c < least) c = least;
+    long long n = (longest + c - 1) / c;
+    if (n > 4 * slots / seq.sequences) n = 4 * slots / seq.sequences;
     if (n < 3) return 1;
-    long long c = (length + n - 1) / n;
+    c = (longest + n - 1) / n;
     c = (c + 31) / 32 * 32;
     *chunk = static_cast<int>(c);
-    return static_cast<int>((length + c - 1) / c);
+    return static_cast<int>((longest + c - 1) / c);
 }
+
+long long all_tokens(const sysscan_args &a) { return a.seq.offsets_dev ? a.seq.total : a.seq.sequences * a.seq.length; }
 
 }  // namespace
 
@@ -36,8 +49,7 @@ ScanPlan scan_plan(const sysscan_args &a)
     // 2560: 308 (four) against 316 us, 4096: 351 against 316, 8192: 517 against 614: four from 1.7 warps a scheduler on.
     p.s = np >= 4 && (np >= 64 || rows * np / (4 * 32) * 10 >= 17 * kSchedulers) ? 4 : 2;
     p.ln = np / p.s;
-    const long long warps = (rows * p.ln + 31) / 32;
-    p.chunks = pick_chunks(warps, a.seq.length, 4 * kSchedulers, &p.chunk);
+    p.chunks = pick_chunks((a.channels * p.ln + 31) / 32, a.seq, all_tokens(a), 128, &p.chunk);
     if (p.chunks > 1) {
         p.carry_floats = a.seq.sequences * p.chunks * a.channels * a.states;
         p.dsum_floats = a.seq.sequences * p.chunks * a.channels;
@@ -57,9 +69,8 @@ ScanBackPlan scan_backward_plan(const sysscan_args &a)
     const int np = padded_states(a.states);
     p.s = np >= 128 ? 4 : 2;
     p.ln = np / p.s;
-    const long long warps = (a.seq.sequences * a.channels * p.ln + 31) / 32;
-    p.chunks = pick_chunks(warps, a.seq.length, 4 * kSchedulers, &p.chunk);
-    const long long total = a.seq.offsets_dev ? a.seq.total : a.seq.sequences * a.seq.length;
+    const long long total = all_tokens(a);
+    p.chunks = pick_chunks((a.channels * p.ln + 31) / 32, a.seq, total, 32, &p.chunk);
     const long long cb = (p.ln <= 16 || np >= 128 ? 256 : 512) / p.ln;    // channels per block
     const long long blocks = (a.channels / a.groups + cb - 1) / cb * a.groups;
     p.bc_floats = blocks * total * 2 * np;
