@@ -9,6 +9,7 @@
 //
 //  * No space (tokens): a block's threads hold whole rows of channels in registers; read once, written once.
 //  * Little space (a warp's registers hold a group), forward: a warp per group; read once, written once.
+//  * A tile of a batch entry fits in a block's shared memory: a block per tile; read once, written once.
 //  * Everything else: partial sums per slab of rows, a small kernel that joins the slabs in a fixed order, and a second
 //    pass.  The second pass walks the slabs from the last to the first: the end of what the first pass read is still
 //    in the 126 MB L2.
@@ -729,6 +730,140 @@ __global__ void __launch_bounds__(kNormThreads) norm_back_join_kernel(NormArgs a
     }
 }
 
+// ---- a block per batch entry and tile: the tile fits in shared memory ---------------------------------------------------------
+// The threads' rows stay in shared memory, each thread's own where only it reads them, between the sums and the second pass:
+// read once, written once, one launch instead of three.
+
+template <typename T, int V, bool BACK>
+struct BlockRoom {
+    static constexpr int STREAMS = BACK ? 2 : 1, PITCH = kNormThreads * V * static_cast<int>(sizeof(T)), SLOT = PITCH * STREAMS;
+    // rows, [2 V][threads] sums, [2][tile] channel sums, [groups of the tile] pairs
+    static __host__ __device__ int sums_at(int rows) { return rows * SLOT; }
+    static __host__ __device__ int chan_at(int rows) { return sums_at(rows) + 2 * V * kNormThreads * 4; }
+    static __host__ __device__ int group_at(int rows, int tile) { return chan_at(rows) + 2 * tile * 4; }
+    static size_t bytes(int rows, int tile, int groups) { return group_at(rows, tile) + groups * 8; }
+};
+
+template <typename T, int V, bool BACK>
+__global__ void __launch_bounds__(kNormThreads) norm_block_kernel(NormArgs a)
+{
+    using G = BlockRoom<T, V, BACK>;
+    extern __shared__ __align__(16) char norm_smem[];
+    dependent_launch_enter();
+    const int tiles = (a.channels + a.tile - 1) / a.tile;
+    const long long b = blockIdx.x / tiles;
+    const int c0 = (blockIdx.x - static_cast<int>(b) * tiles) * a.tile;
+    SlabPlace p;
+    p.b = b;
+    p.c0 = c0;
+    p.channels = min(a.tile, a.channels - c0);
+    p.per_row = p.channels / V;                                          // at most 256
+    p.step = kNormThreads / p.per_row;
+    p.r0 = threadIdx.x / p.per_row;
+    p.cv = threadIdx.x - p.r0 * p.per_row;
+    p.live = p.r0 < p.step;
+    const int space = static_cast<int>(a.space), slots = a.rows_per_slab;     // slots: rows of the thread that has most
+    const int n = p.live && p.r0 < space ? (space - p.r0 + p.step - 1) / p.step : 0;
+    const int c = p.live ? c0 + p.cv * V : c0, g0 = c0 / a.cg, groups = p.channels / a.cg;
+    char *own = norm_smem + threadIdx.x * (V * sizeof(T));
+    const T *px = norm_at<T>(a.x, b, p.r0, c), *pd = BACK ? norm_at<T>(a.dy, b, p.r0, c) : nullptr;
+    const long long sx = p.step * a.x.tstride, sd = p.step * a.dy.tstride;
+    auto fill = [&](char *to, const T *from) {
+        if constexpr (V * sizeof(T) >= 4) copy_async<V * sizeof(T)>(to, from);
+        else store_pack(reinterpret_cast<T *>(to), load_pack<T, V>(from));
+    };
+#pragma unroll 4
+    for (int i = 0; i < n; ++i, px += sx) {
+        fill(own + i * G::SLOT, px);
+        if (BACK) {
+            fill(own + i * G::SLOT + G::PITCH, pd);
+            pd += sd;
+        }
+    }
+    copy_commit();
+    auto x_at = [&](int i) { return widen(load_pack<T, V>(reinterpret_cast<const T *>(own + i * G::SLOT))); };
+    auto dy_at = [&](int i) { return widen(load_pack<T, V>(reinterpret_cast<const T *>(own + i * G::SLOT + G::PITCH))); };
+    const long long bg = b * a.groups;
+    const Vec<V> w = load_params<float, V>(a.w, c, true, false, 1.0f), bias = load_params<float, V>(a.b, c, true, false, 0.0f);
+    Vec<V> mean, rstd, s1 = splat<V>(0.0f), s2 = splat<V>(0.0f);         // mean: negated; forward first the shift
+    if (BACK) {
+        mean = vmul(per_channel<T, V>(c, a.cg, a.mean + bg), splat<V>(-1.0f));
+        rstd = per_channel<T, V>(c, a.cg, a.rstd + bg);
+    } else {
+        mean = each<V>([&](int j) { return -to_f32(*norm_at<T>(a.x, b, 0, (c + j) / a.cg * a.cg)); });
+    }
+    copy_wait<0>();
+    if (BACK) {
+        const Vec<V> scale = vmul(w, rstd);
+        for (int i = 0; i < n; ++i) {
+            const Vec<V> xm = vadd(x_at(i), mean);
+            Vec<V> e = dy_at(i);
+            if (a.silu) e = vmul(e, vsilu_slope(vfma(xm, scale, bias)));
+            s1 = vadd(s1, e);
+            s2 = vfma(e, xm, s2);
+        }
+        s2 = vmul(s2, rstd);
+    } else {
+        for (int i = 0; i < n; ++i) {
+            const Vec<V> v = vadd(x_at(i), mean);
+            s1 = vadd(s1, v);
+            s2 = vfma(v, v, s2);
+        }
+    }
+    float (*sums)[kNormThreads] = reinterpret_cast<float (*)[kNormThreads]>(norm_smem + G::sums_at(slots));
+    float *chan = reinterpret_cast<float *>(norm_smem + G::chan_at(slots));
+    float2 *of_group = reinterpret_cast<float2 *>(norm_smem + G::group_at(slots, a.tile));
+    add_rows<V>(p, s1, s2, sums, chan);
+    const float inv = 1.0f / (static_cast<float>(a.space) * static_cast<float>(a.cg));
+    const int lane = threadIdx.x & 31;
+    for (int g = threadIdx.x >> 5; g < groups; g += kNormThreads / 32) {
+        float2 v = make_float2(0.0f, 0.0f);
+        for (int i = g * a.cg + lane; i < (g + 1) * a.cg; i += 32) {
+            const float scale = BACK && a.w ? a.w[c0 + i] : 1.0f;
+            v.x = fmaf(scale, chan[i], v.x);
+            v.y = fmaf(scale, chan[p.channels + i], v.y);
+        }
+        v = warp_sum(v);
+        if (lane == 0) {
+            v.x *= inv;
+            v.y *= inv;
+            if (!BACK) {
+                v = make_float2(to_f32(*norm_at<T>(a.x, b, 0, c0 + g * a.cg)) + v.x, rsqrtf(fmaxf(fmaf(-v.x, v.x, v.y), 0.0f) + a.eps));
+                if (a.mean) a.mean[bg + g0 + g] = v.x;
+                if (a.rstd) a.rstd[bg + g0 + g] = v.y;
+            }
+            of_group[g] = v;
+        }
+    }
+    if (BACK)
+        for (int q = threadIdx.x; q < 2 * p.channels; q += kNormThreads)
+            a.pq[(b * 2 + q / p.channels) * a.channels + c0 + q % p.channels] = chan[q];
+    __syncthreads();
+    const Tokens &to = BACK ? a.dx : a.y;
+    T *dst = norm_at<T>(to, b, p.r0, c);
+    const long long so = p.step * to.tstride;
+    auto first = [&](int j) { return of_group[(c + j) / a.cg - g0].x; };
+    auto second = [&](int j) { return of_group[(c + j) / a.cg - g0].y; };
+    if (BACK) {
+        const Vec<V> scale = vmul(w, rstd), minus = vmul(rstd, splat<V>(-1.0f));
+        const Vec<V> k1 = vmul(each<V>(first), minus), k2 = vmul(vmul(each<V>(second), minus), rstd);
+        for (int i = 0; i < n; ++i, dst += so) {
+            const Vec<V> xm = vadd(x_at(i), mean);
+            Vec<V> e = dy_at(i);
+            if (a.silu) e = vmul(e, vsilu_slope(vfma(xm, scale, bias)));
+            store_pack(dst, narrow<T, V>(vfma(e, scale, vfma(xm, k2, k1))));
+        }
+    } else {
+        const Vec<V> scale = vmul(w, each<V>(second));
+        mean = vmul(each<V>(first), splat<V>(-1.0f));
+        for (int i = 0; i < n; ++i, dst += so) {
+            Vec<V> v = vfma(vadd(x_at(i), mean), scale, bias);
+            if (a.silu) v = vsilu(v);
+            store_pack(dst, narrow<T, V>(v));
+        }
+    }
+}
+
 // dweight, dbias: sums over the rows of pq.  8 channels x 64 row slices a block: there may be few channels and many rows.
 constexpr int kParamSlices = 64;
 __global__ void __launch_bounds__(8 * kParamSlices) norm_param_kernel(const float *pq, long long rows, int channels, float *dweight, float *dbias)
@@ -764,6 +899,7 @@ struct NormPlan {
     int q;                       // token form: vectors per thread (0: another form)
     int threads, rows, run, blocks;
     int r;                       // warp form: vectors per lane (0: slabs)
+    bool block;                  // block form
     int tile, tiles, rows_per_slab, slabs, entry_step;
     long long part_floats, pq_floats, sum_floats, stat_floats;
 };
@@ -812,8 +948,44 @@ NormPlan norm_plan(const sysgroupnorm_args &a, bool back)
         p.entry_step = static_cast<int>(step < a.batch ? step : a.batch);
         return p;
     }
-    // slabs: a tile is all channels if a row of them has at most 256 vectors, else as many whole groups as do
     const int inside = p.v;
+    // a block per batch entry and tile.  The tile: whole groups, halved while it has no room or the batch alone does not fill
+    // the machine, with at least 64 bytes of a row together.  Room: 64 KB, so that an SM holds several blocks; twice that and more
+    // where there is about one block per SM anyway.  Forward / training step, us, by slabs and by blocks: 4 x 504 x 12 fp32: 8 / 32
+    // and 8 / 24.5; 899 x 13 x 440 fp16: 28 / 92 and 15 / 42; 2200 x 33 x 448 fp16: 102 / - and 50 / 158; 4 x 1024 x 1280 bf16: 21 / 57
+    // and 10 / 29; 300 x 400 x 320 bf16: 68 / 208 and 50 / 171 (73 / 203 with 196 KB); 1 x 4096 x 320 bf16, 8 blocks of 196 KB: 16 / 29
+    // against 12 / 28 by slabs.
+    {
+        int v = 4;
+        while (v > 1 && (a.channels % v != 0 || !aligned(v))) v /= 2;
+        long long most = a.groups;                                       // groups of a tile
+        if (a.channels > kNormThreads * v) {
+            v = inside < 4 ? inside : 4;
+            most = kNormThreads * v / cg;
+        }
+        auto data = [&](long long tg) {                                  // bytes of the rows of the threads
+            const long long step = kNormThreads / (tg * cg / v);
+            return (a.space + step - 1) / step * kNormThreads * v * static_cast<long long>(esz) * (back ? 2 : 1);
+        };
+        auto blocks = [&](long long tg) { return a.batch * ((a.groups + tg - 1) / tg); };
+        auto fits = [&](long long tg) { return data(tg) <= (blocks(tg) >= 64 && blocks(tg) <= 148 ? 196 : 64) * 1024; };
+        while (most > 1 && (!fits(most) || blocks(most) < 148)) {
+            const long long half = (most + 1) / 2;
+            if (half * cg % v != 0 || half * cg * static_cast<long long>(esz) < 64) break;
+            most = half;
+        }
+        if (most > 0 && a.space <= 196 * 1024 && fits(most) && blocks(most) < 0x7fffffff) {
+            p.v = v;
+            p.block = true;
+            p.tile = static_cast<int>(most * cg);
+            p.tiles = static_cast<int>((a.groups + most - 1) / most);
+            const long long step = kNormThreads / (p.tile / v);
+            p.rows_per_slab = ceil_div(a.space, step);                   // of a thread
+            if (back) p.pq_floats = a.batch * 2 * a.channels;
+            return p;
+        }
+    }
+    // slabs: a tile is all channels if a row of them has at most 256 vectors, else as many whole groups as do
     p.v = widest;
     while (p.v > 1 && (a.channels % p.v != 0 || !aligned(p.v))) p.v /= 2;
     long long tile = a.channels;
@@ -917,6 +1089,15 @@ cudaError_t launch_norm_tokens(const NormArgs &k, const NormPlan &p, cudaStream_
     }
 }
 
+template <typename T, int V, bool BACK>
+cudaError_t launch_norm_block(const NormArgs &k, const NormPlan &p, cudaStream_t s)
+{
+    if constexpr (V > 4) return kNoInstantiation;
+    else
+        return launch_kernel_smem(norm_block_kernel<T, V, BACK>, dim3(static_cast<unsigned>(k.batch * p.tiles)), dim3(kNormThreads),
+                                  BlockRoom<T, V, BACK>::bytes(p.rows_per_slab, p.tile, p.tile / k.cg), s, k);
+}
+
 // batch entries go out 65535 at a time: the grid's limit
 template <typename F>
 cudaError_t by_entries(NormArgs k, size_t esz, F f)
@@ -958,8 +1139,9 @@ cudaError_t launch_groupnorm(const sysgroupnorm_args &a, cudaStream_t s, int *la
         using T = std::remove_pointer_t<decltype(tag)>;
         return with_width<T>(p.v, [&](auto width) -> cudaError_t {
             constexpr int V = decltype(width)::value;
-            if (p.q > 0 || p.r > 0) {
+            if (p.q > 0 || p.r > 0 || p.block) {
                 *launches += 1;
+                if (p.block) return launch_norm_block<T, V, false>(k, p, s);
                 return p.q > 0 ? launch_norm_tokens<T, V, false>(k, p, s) : launch_norm_warp<T, V>(k, p, s);
             }
             float *stats = k.part + p.part_floats;
@@ -987,9 +1169,9 @@ cudaError_t launch_groupnorm_backward(const sysgroupnorm_args &a, cudaStream_t s
         using T = std::remove_pointer_t<decltype(tag)>;
         return with_width<T>(p.v, [&](auto width) -> cudaError_t {
             constexpr int V = decltype(width)::value;
-            if (p.q > 0) {
+            if (p.q > 0 || p.block) {
                 *launches += 1;
-                return launch_norm_tokens<T, V, true>(k, p, s);
+                return p.block ? launch_norm_block<T, V, true>(k, p, s) : launch_norm_tokens<T, V, true>(k, p, s);
             }
             return by_entries(k, sizeof(T), [&](NormArgs q, long long b0) {
                 q.part = k.part + b0 * k.slabs * 2 * k.channels;

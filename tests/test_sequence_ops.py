@@ -473,6 +473,31 @@ def test_norm_forward_and_backward(cuda_device, case):
         close(db, k["db"], k["db_mag"] * (1 + np.max(mag)), 2.0 ** -14, "dbias")
 
 
+NORM_TILES = [
+    ("bf16", 3, (50,), 448, 7, True, True),         # tiles of four groups and of three
+    ("f16", 200, (12,), 24, 1, True, True),
+    ("bf16", 150, (13,), 440, 8, True, False),
+    ("f32", 70, (100,), 600, 3, True, True),        # more than 64 KB a tile
+    ("f16", 5, (31,), 9, 3, True, True),            # one channel an access, of 16 bits
+    ("bf16", 2, (90, 80), 23, 1, True, True),       # slabs, one channel an access
+    ("bf16", 1, (700,), 4096, 8, True, True),       # slabs, several tiles of channels
+    ("f32", 2, (40, 40), 1030, 5, False, True),
+]
+
+
+@pytest.mark.parametrize("case", NORM_TILES, ids=str)
+def test_norm_tiles_and_slabs(cuda_device, case):
+    test_norm_forward_and_backward(cuda_device, case)
+
+
+def test_norm_leaves_its_inputs(cuda_device):
+    x, dy, g, w, b, act = norm_case(NORM_TILES[0])
+    kept = x.clone(), dy.clone()
+    y, mean, rstd = seq.groupnorm(x, g, w, b, activation=act, return_stats=True)
+    seq.groupnorm_backward(dy, x, g, mean, rstd, w, b, act)
+    assert torch.equal(x, kept[0]) and torch.equal(dy, kept[1])
+
+
 def test_norm_mean_far_from_zero_and_constant_groups(cuda_device):
     """A mean 1000 deviations away costs no digits beyond those of the inputs; a constant group has variance 0."""
     x = (Draw(1, torch.float32)(3, 500, 32) + 1000.0)
