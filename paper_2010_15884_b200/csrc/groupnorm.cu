@@ -864,8 +864,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_block_kernel(NormArgs a)
     }
 }
 
-// dweight, dbias: sums over the rows of pq.  8 channels x 64 row slices a block: there may be few channels and many rows.
-constexpr int kParamSlices = 64;
+// dweight, dbias: sums over the rows of pq.  8 channels x 128 row slices a block: there may be few channels and many rows.
+constexpr int kParamSlices = 128;
 __global__ void __launch_bounds__(8 * kParamSlices) norm_param_kernel(const float *pq, long long rows, int channels, float *dweight, float *dbias)
 {
     dependent_launch_enter();
@@ -873,7 +873,7 @@ __global__ void __launch_bounds__(8 * kParamSlices) norm_param_kernel(const floa
     const int c = blockIdx.x * 8 + threadIdx.x;
     float2 v = make_float2(0.0f, 0.0f);
     if (c < channels)
-#pragma unroll 4
+#pragma unroll 8
         for (long long r = threadIdx.y; r < rows; r += kParamSlices) {
             v.x += pq[r * 2 * channels + c];
             v.y += pq[(r * 2 + 1) * channels + c];
