@@ -454,7 +454,9 @@ __global__ void __launch_bounds__(kBlockThreads, 2) scan_kernel(ScanArgs a)
     }
 }
 
-// Chains the chunks: the state each chunk starts from.  One thread per (sequence, channel, state).
+// Chains the chunks: the state each chunk starts from.  One thread per (sequence, channel, state); the loads of kChainAhead
+// chunks go out together.
+constexpr int kChainAhead = 8;
 static __global__ void scan_chain_kernel(ScanArgs a)
 {
     dependent_launch_enter();
@@ -466,13 +468,23 @@ static __global__ void scan_chain_kernel(ScanArgs a)
     const long long length = a.map.end(r) - a.map.first(r);
     float h = a.state ? a.state[id] : 0.0f;
     const float A = decay_rate(a.A[e]);
-    for (int k = 0; k < a.chunks && (k == 0 || static_cast<long long>(k) * a.chunk < length); ++k) {
-        const long long chain = static_cast<long long>(r) * a.chunks + k;
-        const bool more = k + 1 < a.chunks && static_cast<long long>(k + 1) * a.chunk < length;   // the last one left nothing
-        const float last = more ? a.carry[chain * cn + e] : 0.0f;
-        const float sum = more ? a.dsum[chain * a.channels + c] : 0.0f;
-        a.carry[chain * cn + e] = h;
-        h = fmaf(exp2_fast(A * sum), h, last);
+    const int used = length <= 0 ? 1 : static_cast<int>(min(static_cast<long long>(a.chunks), (length + a.chunk - 1) / a.chunk));
+    float *carry = a.carry + static_cast<long long>(r) * a.chunks * cn + e;
+    const float *dsum = a.dsum + static_cast<long long>(r) * a.chunks * a.channels + c;
+    for (int k0 = 0; k0 < used; k0 += kChainAhead) {
+        float last[kChainAhead], decay[kChainAhead];
+#pragma unroll
+        for (int i = 0; i < kChainAhead; ++i) {
+            const int k = k0 + i;
+            const bool more = k + 1 < used;                              // the last one left nothing
+            last[i] = more ? carry[static_cast<long long>(k) * cn] : 0.0f;
+            decay[i] = more ? dsum[static_cast<long long>(k) * a.channels] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kChainAhead; ++i) {
+            if (k0 + i < used) carry[static_cast<long long>(k0 + i) * cn] = h;
+            h = fmaf(exp2_fast(A * decay[i]), h, last[i]);
+        }
     }
 }
 

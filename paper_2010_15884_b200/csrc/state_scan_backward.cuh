@@ -418,11 +418,21 @@ static __global__ void scan_chain_back_kernel(ScanBackArgs b)
     float carry = b.dfinal ? b.dfinal[id] : 0.0f;
     const float A = decay_rate(a.A[e]);
     const long long used = length <= 0 ? 1 : min(static_cast<long long>(a.chunks), (length + a.chunk - 1) / a.chunk);
-    for (long long k = used - 1; k >= 0; --k) {
-        const long long chain = static_cast<long long>(r) * a.chunks + k;
-        const float local = k > 0 ? a.carry[chain * cn + e] : 0.0f, sum = k > 0 ? a.dsum[chain * a.channels + c] : 0.0f;
-        a.carry[chain * cn + e] = carry;
-        carry = fmaf(exp2_fast(A * sum), carry, local);
+    float *at = a.carry + static_cast<long long>(r) * a.chunks * cn + e;
+    const float *dsum = a.dsum + static_cast<long long>(r) * a.chunks * a.channels + c;
+    for (int k0 = static_cast<int>(used) - 1; k0 >= 0; k0 -= kChainAhead) {
+        float local[kChainAhead], decay[kChainAhead];
+#pragma unroll
+        for (int i = 0; i < kChainAhead; ++i) {
+            const int k = k0 - i;
+            local[i] = k > 0 ? at[static_cast<long long>(k) * cn] : 0.0f;
+            decay[i] = k > 0 ? dsum[static_cast<long long>(k) * a.channels] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kChainAhead; ++i) {
+            if (k0 - i >= 0) at[static_cast<long long>(k0 - i) * cn] = carry;
+            carry = fmaf(exp2_fast(A * decay[i]), carry, local[i]);
+        }
     }
 }
 
@@ -468,18 +478,25 @@ __global__ void __launch_bounds__(256) scan_bc_kernel(ScanBackArgs b)
     }
 }
 
-// dA, dD, ddelta_bias: column sums of par_part over sequences and chunks.
+// dA, dD, ddelta_bias: column sums of par_part over sequences and chunks.  32 columns x 8 row slices a block.
 static __global__ void __launch_bounds__(256) scan_param_kernel(ScanBackArgs b)
 {
     dependent_launch_enter();
+    __shared__ float sums[8][32];
     const ScanArgs &a = b.f;
     const long long columns = static_cast<long long>(a.channels) * (a.states + 2);
-    const long long col = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    if (col >= columns) return;
+    const int lane = threadIdx.x % 32, slice = threadIdx.x / 32;
+    const long long col = static_cast<long long>(blockIdx.x) * 32 + lane;
     const long long rows = static_cast<long long>(a.map.sequences) * a.chunks;
     float v = 0.0f;
-#pragma unroll 4
-    for (long long i = 0; i < rows; ++i) v += b.par_part[i * columns + col];
+    if (col < columns)
+#pragma unroll 8
+        for (long long i = slice; i < rows; i += 8) v += b.par_part[i * columns + col];
+    sums[slice][lane] = v;
+    __syncthreads();
+    if (slice > 0 || col >= columns) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += sums[i][lane];
     const long long cn = static_cast<long long>(a.channels) * a.states;
     if (col < cn) {
         if (b.dA) b.dA[col] = v;
@@ -534,7 +551,7 @@ cudaError_t launch_scan_backward_shape(ScanBackArgs b, cudaStream_t s, int *laun
         *launches += 1;
     }
     *launches += 1;
-    return launch_kernel(scan_param_kernel, dim3(ceil_div(static_cast<long long>(b.f.channels) * (b.f.states + 2), 256)), dim3(256), s, b);
+    return launch_kernel(scan_param_kernel, dim3(ceil_div(static_cast<long long>(b.f.channels) * (b.f.states + 2), 32)), dim3(256), s, b);
 }
 
 template <typename T>

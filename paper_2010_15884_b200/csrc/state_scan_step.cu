@@ -9,8 +9,8 @@ constexpr long long kSchedulers = 148 * 4;
 
 // Chunks per sequence.  `warps` = warps that one sequence takes unsplit.  A chunk costs a second pass over its tokens, so tokens
 // are split only while the machine would be mostly idle, into chunks that fill four warps a scheduler.  8192 tokens and 16 states,
-// by channels, whole against split, forward: 256: 198 / 48 us, 1024: 237 / 132, 1408: 240 / 165, 2048: 243 / 242; training step:
-// 256: 1818 / 151, 768: 1852 / 362; with six or eight warps a scheduler 256 channels take 176 or 183 us.
+// by channels, whole against split, forward: 256: 198 / 40 us, 1024: 237 / 130, 1408: 240 / 164, 2048: 243 / 242; training step:
+// 256: 1818 / 134, 768: 1852 / 362.
 // Never finer than `least` tokens: forward 128, backward 32, where a token takes longer (300 tokens of 2000 channels forward:
 // 10.6 us whole, 20 in chunks of 32; training step of 342 tokens of 432 channels: 78 whole, 51 in chunks of 32).
 // Sequences may differ in length, so the chunk follows from all tokens, less one part-filled chunk per sequence (four packed
