@@ -3,7 +3,7 @@
 //   pre[t] = bias + sum_{k<K} w[k] line[t+k],  line = state ++ x,  y = act(pre)
 //
 // Bound: memory.  An output costs K multiply-adds and one exp / division pair against 4 bytes (16-bit tokens), so the
-// kernels are built around the traffic: a thread owns V neighbouring channels (16 bytes) and walks along the tokens with
+// kernels are built around the traffic: a thread owns V neighbouring channels (four where rows allow) and walks along the tokens with
 // the last K-1 inputs in registers, as the output-stationary array does with its forwarded inputs; only a run's first
 // K-1 rows are read twice.  Runs are cut short when there are too few of them to fill the machine.
 #include "seq_common.cuh"
